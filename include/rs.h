@@ -26,7 +26,7 @@
  *     kernel is launched and leave the device untouched; rs_last_error() gives
  *     a message for the calling thread's most recent failure.
  *   - Same inputs give bit-identical outputs (no floating-point atomics).
- *   - Alignment: every tensor pointer must be 16-byte aligned.
+ *   - Alignment: every tensor pointer must be 16-byte aligned (row statistics and per-row scales: as their calls say).
  */
 #ifndef RS_H
 #define RS_H
@@ -270,6 +270,73 @@ RS_API rs_status rs_pack_linear(const void *w, void *wt, int32_t K, int32_t N, r
 RS_API rs_status rs_linear_fwd(const void *a, const void *w, const void *bias, const void *res,
                                void *out, int64_t M, int32_t N, int32_t K, rs_epilogue epi,
                                rs_dtype dtype, void *hip_stream);
+
+/*
+ * Linear layers in 8-bit integers (W8A8): integers with one scale for each token (row of the activations) and each output channel
+ * (column of the weights),
+ *     out[m, n] = epilogue( (sum_k a[m, k] w[k, n]) * a_scale[m] * w_scale[n] + bias[n] )
+ * the sum exact in 32-bit integers, all behind it in fp32, rounded to the output type once.  Epilogues as in rs_linear_fwd.
+ *
+ * rs_quantize_rows forms 8-bit rows from fp32 or bf16 ones, symmetric about zero:
+ *     scale[m] = max(max_k |x[m, k]| * (1 / 127), FLT_MIN),   q[m, k] = round(x[m, k] * (1 / scale[m]))
+ *   each operation in fp32, halves to even: the same integers whatever ran.  A row that holds an infinity or a NaN gets scale NaN
+ *   and zeros, so that a layer's output row is NaN.
+ *   x : element (m, k) at m * ldx + k (elements; ldx >= K).   q : (m, k) at m * ldq + k; ldq >= K, a multiple of 16.
+ *   Bytes K .. (K rounded up to 16) - 1 of a row of q are written as zeros, those behind them are left alone.   scale : float [M].
+ * rs_quantize_columns does the same to the columns of a weight matrix w [K, N] (fp32 or bf16): q [K, N], scale [N].
+ * rs_pack_linear_i8 lays weights q [K, N] (any int8 values) out as the kernels read them: rs_packed_linear_i8_size(K, N) bytes
+ *   (0 for sizes that rs_linear_i8_fwd refuses), every one of them written.  Layout of this library version, as rs_pack_weights.
+ * rs_linear_i8_fwd:
+ *   a : int8 (m, k) at m * lda + k, lda >= K and a multiple of 16; all M rows have lda bytes of memory.  Bytes behind column K
+ *       may hold anything.        a_scale : float [M].       w : packed weights.      w_scale : float [N].
+ *   bias : [N] or NULL;  res : [M, N] for RS_EPI_BIAS_RES;  out : [M, N], all in `dtype`.  out may be res; it must not overlap
+ *       anything else.            K <= 131071, N <= 2^20, both otherwise any size; M < 2^31.
+ * a_scale and scale must be 4-byte aligned, everything else 16-byte.  No workspace.  Deterministic.
+ */
+RS_API rs_status rs_quantize_rows(const void *x, int64_t M, int32_t K, int64_t ldx, rs_dtype dtype, int8_t *q, int64_t ldq,
+                                  float *scale, void *hip_stream);
+RS_API rs_status rs_quantize_columns(const void *w, int32_t K, int32_t N, rs_dtype dtype, int8_t *q, float *scale,
+                                     void *hip_stream);
+RS_API size_t rs_packed_linear_i8_size(int32_t K, int32_t N);
+RS_API rs_status rs_pack_linear_i8(const int8_t *q, void *packed, int32_t K, int32_t N, void *hip_stream);
+RS_API rs_status rs_linear_i8_fwd(const int8_t *a, int64_t lda, const float *a_scale, const void *w, const float *w_scale,
+                                  const void *bias, const void *res, void *out, int64_t M, int32_t N, int32_t K,
+                                  rs_epilogue epi, rs_dtype dtype, void *hip_stream);
+
+/*
+ * The step between two branches (attention, MLP) of an encoder block, in one pass: the norm behind a branch with its gate and
+ * residual scale, the residual add, and the norm in front of the next branch with its modulation:
+ *     y = x_scale * x + f_scale * gate . Norm_post(f)
+ *     u = Norm_pre(y) . (1 + mod_scale) + mod_shift
+ *   Norm: RS_NORM_NONE, RS_NORM_LAYER ((v - mean) / sqrt(population variance + eps) . g + b) or RS_NORM_RMS
+ *   (v / sqrt(mean of v^2 + eps) . g + b), over the D channels, statistics in fp32.  y enters the second norm as it is
+ *   in fp32, before it is rounded for memory.
+ *   x : [B, N, D], the residual stream.      f : [B, N, D], the branch's output, or NULL (no branch: y = x_scale * x).
+ *   y, u : [B, N, D] out, each may be NULL.
+ *   u_q, u_scale : u as 8-bit rows for rs_linear_i8_fwd by the rule of rs_quantize_rows (from u in fp32): int8 [B * N] rows of
+ *       ldq bytes (ldq >= D, a multiple of 16) and float [B * N]; both or neither NULL.  At least one of y, u, u_q is wanted.
+ *   y may be x, u may be f; otherwise no output overlaps anything.
+ * Vectors (rs_residual_norm_weights, element type cfg->dtype, NULL: g and gate 1, the others 0): post_g, post_b, pre_g and
+ *   pre_b are [D]; gate is read at image * gate_stride, mod_scale and mod_shift at image * mod_stride (elements; 0: one
+ *   vector for all images).  post_g, post_b and gate must be NULL if f is, and the two vectors of a norm if it is RS_NORM_NONE.
+ * D % 8 == 0, D <= 16384, strides multiples of 8 (>= 0), B * N < 2^31, eps > 0 for a norm that is taken.  u_scale must be 4-byte
+ * aligned.  No workspace.  Deterministic.
+ */
+typedef enum { RS_NORM_NONE = 0, RS_NORM_LAYER = 1, RS_NORM_RMS = 2 } rs_norm;
+typedef struct {
+    int32_t B, N, D;
+    rs_norm post, pre;
+    float post_eps, pre_eps;
+    float x_scale, f_scale;
+    rs_dtype dtype;
+    int64_t gate_stride, mod_stride;
+} rs_residual_norm_cfg;
+typedef struct {
+    const void *post_g, *post_b, *gate, *pre_g, *pre_b, *mod_scale, *mod_shift;
+} rs_residual_norm_weights;
+RS_API rs_status rs_residual_norm_fwd(const rs_residual_norm_cfg *cfg, const rs_residual_norm_weights *w, const void *x,
+                                      const void *f, void *y, void *u, int8_t *u_q, int64_t ldq, float *u_scale,
+                                      void *hip_stream);
 
 /*
  * One pre-LN encoder block followed by representation-shift pruning

@@ -21,11 +21,14 @@ RS_SHIFT_MLP, RS_SHIFT_ATTN, RS_SHIFT_BLOCK, RS_SHIFT_MLP_STREAM, RS_SHIFT_MLP_N
 
 RS_PROFILE_CLASSES = 11
 RS_EPI_BIAS, RS_EPI_BIAS_GELU, RS_EPI_BIAS_RES = 0, 1, 2
+RS_NORM_NONE, RS_NORM_LAYER, RS_NORM_RMS = 0, 1, 2
 
 EXPORTS = ("rs_last_error", "rs_version", "rs_build_info", "rs_tune_gemm_variant", "rs_profile_enable", "rs_profile_read",
            "rs_profile_class_name", "rs_attention_fwd", "rs_attention_map_size",
            "rs_attention_map_workspace_size", "rs_attention_map_fwd", "rs_shift_topk_workspace_size",
-           "rs_shift_topk", "rs_grid_line_prune", "rs_grid_token_prune", "rs_pack_linear", "rs_linear_fwd", "rs_packed_weights_size", "rs_pack_weights", "rs_block_workspace_size",
+           "rs_shift_topk", "rs_grid_line_prune", "rs_grid_token_prune", "rs_pack_linear", "rs_linear_fwd",
+           "rs_quantize_rows", "rs_quantize_columns", "rs_packed_linear_i8_size", "rs_pack_linear_i8", "rs_linear_i8_fwd",
+           "rs_residual_norm_fwd", "rs_packed_weights_size", "rs_pack_weights", "rs_block_workspace_size",
            "rs_block_fwd", "rs_block_fwd_chained", "rs_block_static_scratch_size", "rs_block_fwd_static")
 
 _vp = ctypes.c_void_p
@@ -43,6 +46,16 @@ class RsBlockCfg(ctypes.Structure):
                 ("n_prefix", _i32), ("n_keep", _i32), ("ln_eps", ctypes.c_float),
                 ("attn_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("dist", ctypes.c_int),
                 ("op", ctypes.c_int)]
+
+
+class RsResidualNormWeights(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("post_g", "post_b", "gate", "pre_g", "pre_b", "mod_scale", "mod_shift")]
+
+
+class RsResidualNormCfg(ctypes.Structure):
+    _fields_ = [("B", _i32), ("N", _i32), ("D", _i32), ("post", ctypes.c_int), ("pre", ctypes.c_int),
+                ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float), ("x_scale", ctypes.c_float),
+                ("f_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("gate_stride", _i64), ("mod_stride", _i64)]
 
 
 class RsError(RuntimeError):
@@ -98,6 +111,19 @@ def lib():
         L.rs_grid_token_prune.restype = ctypes.c_int
         L.rs_linear_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, ctypes.c_int, ctypes.c_int, _vp]
         L.rs_linear_fwd.restype = ctypes.c_int
+        L.rs_quantize_rows.argtypes = [_vp, _i64, _i32, _i64, ctypes.c_int, _vp, _i64, _vp, _vp]
+        L.rs_quantize_rows.restype = ctypes.c_int
+        L.rs_quantize_columns.argtypes = [_vp, _i32, _i32, ctypes.c_int, _vp, _vp, _vp]
+        L.rs_quantize_columns.restype = ctypes.c_int
+        L.rs_packed_linear_i8_size.argtypes = [_i32, _i32]
+        L.rs_packed_linear_i8_size.restype = ctypes.c_size_t
+        L.rs_pack_linear_i8.argtypes = [_vp, _vp, _i32, _i32, _vp]
+        L.rs_pack_linear_i8.restype = ctypes.c_int
+        L.rs_linear_i8_fwd.argtypes = [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, ctypes.c_int, ctypes.c_int, _vp]
+        L.rs_linear_i8_fwd.restype = ctypes.c_int
+        L.rs_residual_norm_fwd.argtypes = [ctypes.POINTER(RsResidualNormCfg), ctypes.POINTER(RsResidualNormWeights),
+                                           _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp]
+        L.rs_residual_norm_fwd.restype = ctypes.c_int
         L.rs_packed_weights_size.argtypes = [ctypes.POINTER(RsBlockCfg)]
         L.rs_packed_weights_size.restype = ctypes.c_size_t
         L.rs_pack_weights.argtypes = [ctypes.POINTER(RsBlockCfg), ctypes.POINTER(RsBlockWeights), _vp, _vp]
@@ -263,6 +289,103 @@ def rs_linear_fwd(a, w, bias, res, out, epi=RS_EPI_BIAS, stream=None) -> None:
     N = out.shape[1]
     _check(lib().rs_linear_fwd(_ptr(a), _ptr(w), _ptr(bias), _ptr(res), _ptr(out), M, N, K, epi,
                                dtype_code(a.dtype), _stream(stream)))
+
+
+def _here(*tensors):
+    """All on the current device, whose current stream the call goes to."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device.index == dev), "every tensor must be on the current device"
+
+
+def rs_quantize_rows(x, q, scale, stream=None) -> None:
+    """x [M, K] (rows any distance apart) -> q int8 [M, K] in rows a multiple of 16 bytes apart, scale float [M]."""
+    M, K = x.shape
+    _here(x, q, scale)
+    assert q.shape == x.shape and q.dtype == torch.int8 and scale.numel() == M and scale.dtype == torch.float32
+    assert x.stride(1) == 1 or K == 1, "the channels of a row must be contiguous"
+    assert q.stride(1) == 1 or K == 1, "the channels of a row must be contiguous"
+    assert scale.is_contiguous()
+    _check(lib().rs_quantize_rows(_ptr(x), M, K, x.stride(0) if M > 1 else max(K, x.stride(0)), dtype_code(x.dtype), _ptr(q),
+                                  _pitch8(q), _ptr(scale), _stream(stream)))
+
+
+def _pitch8(q):
+    """Bytes between the rows of an int8 [M, K] tensor; a single row may say anything."""
+    M, K = q.shape
+    return q.stride(0) if M > 1 else max(q.stride(0), (K + 15) // 16 * 16) // 16 * 16
+
+
+def rs_quantize_columns(w, q, scale, stream=None) -> None:
+    """w [K, N] -> q int8 [K, N], scale float [N]."""
+    K, N = w.shape
+    _here(w, q, scale)
+    assert q.shape == w.shape and q.dtype == torch.int8 and scale.numel() == N and scale.dtype == torch.float32
+    assert w.is_contiguous() and q.is_contiguous() and scale.is_contiguous()
+    _check(lib().rs_quantize_columns(_ptr(w), K, N, dtype_code(w.dtype), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def rs_packed_linear_i8_size(K, N) -> int:
+    return int(lib().rs_packed_linear_i8_size(K, N))
+
+
+def rs_pack_linear_i8(q, packed, stream=None) -> None:
+    """q int8 [K, N] -> packed (rs_packed_linear_i8_size(K, N) bytes)."""
+    K, N = q.shape
+    _here(q, packed)
+    assert q.dtype == torch.int8 and q.is_contiguous()
+    assert packed.numel() * packed.element_size() >= rs_packed_linear_i8_size(K, N) and packed.is_contiguous()
+    _check(lib().rs_pack_linear_i8(_ptr(q), _ptr(packed), K, N, _stream(stream)))
+
+
+def rs_linear_i8_fwd(a, a_scale, w, w_scale, bias, res, out, epi=RS_EPI_BIAS, stream=None) -> None:
+    """out [M, N] = epilogue((a @ W) a_scale w_scale + bias); a int8 [M, K] in rows a multiple of 16 bytes apart, w packed,
+    a_scale float [M], w_scale float [N]; bias, res and out of one type, which is fp32 or bf16."""
+    M, K = a.shape
+    N = out.shape[1]
+    _here(a, a_scale, w, w_scale, bias, res, out)
+    assert a.dtype == torch.int8 and (a.stride(1) == 1 or K == 1), "a is int8 with contiguous channels"
+    assert out.shape == (M, N) and out.is_contiguous()
+    assert a_scale.numel() == M and w_scale.numel() == N and a_scale.dtype == w_scale.dtype == torch.float32
+    assert a_scale.is_contiguous() and w_scale.is_contiguous()
+    assert w.numel() * w.element_size() >= rs_packed_linear_i8_size(K, N), "w is not packed for this K and N"
+    assert bias is None or (bias.numel() == N and bias.dtype == out.dtype and bias.is_contiguous())
+    assert res is None or (res.shape == out.shape and res.dtype == out.dtype and res.is_contiguous())
+    _check(lib().rs_linear_i8_fwd(_ptr(a), _pitch8(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(res), _ptr(out),
+                                  M, N, K, epi, dtype_code(out.dtype), _stream(stream)))
+
+
+def make_residual_norm_cfg(B, N, D, dtype, post=RS_NORM_NONE, pre=RS_NORM_LAYER, post_eps=1e-6, pre_eps=1e-6, x_scale=1.0,
+                           f_scale=1.0, gate_stride=0, mod_stride=0) -> RsResidualNormCfg:
+    code = dtype if isinstance(dtype, int) else dtype_code(dtype)
+    return RsResidualNormCfg(B, N, D, post, pre, post_eps, pre_eps, x_scale, f_scale, code, gate_stride, mod_stride)
+
+
+def make_residual_norm_weights(w: dict) -> RsResidualNormWeights:
+    """w: name -> device tensor (or None) for the vectors of rs_residual_norm_weights, in the type of the configuration; [D], or
+    rows for the images whose distance is the configuration's gate_stride or mod_stride.  The tensors stay alive with the result."""
+    s = RsResidualNormWeights()
+    s.tensors = [w.get(name) for name, _ in RsResidualNormWeights._fields_]
+    _here(*s.tensors)
+    assert all(t is None or t.stride(-1) == 1 for t in s.tensors), "the channels of a vector must be contiguous"
+    assert len({t.dtype for t in s.tensors if t is not None}) <= 1, "the vectors must be of one type"
+    for name, _ in RsResidualNormWeights._fields_:
+        setattr(s, name, _ptr(w.get(name)))
+    return s
+
+
+def rs_residual_norm_fwd(cfg: RsResidualNormCfg, weights: RsResidualNormWeights, x, f, y, u, u_q=None, u_scale=None,
+                         stream=None) -> None:
+    """y = x_scale x + f_scale gate Norm_post(f), u = Norm_pre(y) (1 + mod_scale) + mod_shift; x, f, y, u: [B, N, D] (f, y, u may
+    be None), u_q int8 [B * N, D] in rows a multiple of 16 bytes apart with u_scale float [B * N], or None."""
+    numel = cfg.B * cfg.N * cfg.D
+    _here(x, f, y, u, u_q, u_scale)
+    for t in (x, f, y, u):
+        assert t is None or (t.numel() == numel and t.is_contiguous() and dtype_code(t.dtype) == cfg.dtype)
+    assert u_q is None or (u_q.shape == (cfg.B * cfg.N, cfg.D) and u_q.dtype == torch.int8 and u_q.stride(1) == 1)
+    assert u_scale is None or (u_scale.numel() == cfg.B * cfg.N and u_scale.dtype == torch.float32 and u_scale.is_contiguous())
+    _check(lib().rs_residual_norm_fwd(ctypes.byref(cfg), ctypes.byref(weights), _ptr(x), _ptr(f), _ptr(y), _ptr(u), _ptr(u_q),
+                                      0 if u_q is None else _pitch8(u_q), _ptr(u_scale), _stream(stream)))
 
 
 def rs_packed_weights_size(cfg: RsBlockCfg) -> int:

@@ -323,6 +323,47 @@ hipError_t launch_attn_map_scores(const void* map, float* partial, float* s_cls,
 hipError_t launch_attn_unpack(const void* oh, void* o, int B, int H, int N, int64_t osb, int64_t osn, int64_t osh,
                               hipStream_t s);
 
+// 8-bit rows and columns with one scale each (quantize.hpp has the rule): q [M, K] in rows of ldq bytes, zeros behind column K up to
+// a multiple of 16; q [K, N].
+hipError_t launch_quantize_rows(rs_dtype dt, const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t M, int K,
+                                hipStream_t s);
+hipError_t launch_quantize_columns(rs_dtype dt, const void* w, int8_t* q, float* scale, int K, int N, hipStream_t s);
+
+// out[M, N] = epilogue((a @ w) a_scale w_scale + bias), a in 8-bit rows of lda bytes, w packed (packed_i8_size bytes); EPI_BIAS,
+// EPI_BIAS_GELU and EPI_BIAS_RES.  K <= kGemmI8MaxK: sums of products of -128 .. 127 stay below 2^31.
+struct GemmI8Args {
+    const int8_t* a;
+    int64_t lda;
+    const float* a_scale;
+    const void* w;
+    const float* w_scale;
+    const void *bias, *res;
+    void* out;
+    int64_t M;
+    int N, K;
+};
+constexpr int kGemmI8MaxK = 131071;
+constexpr int kGemmI8MaxPitch = 1 << 21;  // 256 rows of a tile: under 2^30 bytes
+size_t packed_i8_size(int K, int N);
+hipError_t launch_pack_i8(const int8_t* q, void* packed, int K, int N, hipStream_t s);
+hipError_t launch_gemm_i8(rs_dtype dt, GemmEpilogue epi, const GemmI8Args& g, hipStream_t s);
+
+// y = x_scale x + f_scale gate . Norm_post(f), u = Norm_pre(y) . (1 + mod_scale) + mod_shift over rows of D (D % 8 == 0,
+// D <= kResidualNormMaxD), N rows per image; f, y, u and u_q (with u_scale, rows of ldq bytes) and every vector may be null.
+struct ResidualNormArgs {
+    const void *x, *f;
+    const void *post_g, *post_b, *gate, *pre_g, *pre_b, *mod_scale, *mod_shift;
+    void *y, *u;
+    int8_t* u_q;
+    float* u_scale;
+    int64_t rows, gate_stride, mod_stride, ldq;
+    int N, D;
+    rs_norm post, pre;
+    float post_eps, pre_eps, x_scale, f_scale;
+};
+constexpr int kResidualNormMaxD = 16384;
+hipError_t launch_residual_norm(rs_dtype dt, const ResidualNormArgs& p, hipStream_t s);
+
 // bf16 [K, N] row-major -> [N, K] row-major
 hipError_t launch_pack_transpose(const void* w, void* wt, int K, int N, hipStream_t s);
 // bf16 [K, N] row-major (multiples of 64) -> fragment order (frag_off); with `gamma` ([K] bf16) row k is scaled by gamma[k]

@@ -587,6 +587,143 @@ rs_status rs_linear_fwd(const void* a, const void* w, const void* bias, const vo
     return RS_OK;
 }
 
+// ---- 8-bit linear layers ------------------------------------------------------
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// Bytes from the first to the last element of `rows` rows of `width` bytes, `pitch` bytes apart.
+static size_t span(int64_t rows, int64_t pitch, int64_t width) { return rows > 0 ? (size_t)((rows - 1) * pitch + width) : 0; }
+// A row pitch of at most 2^31 - 1 elements: spans of 2^31 rows stay below 2^63 bytes.
+constexpr int64_t kMaxPitch = ((int64_t)1 << 29) - 1;
+
+rs_status rs_quantize_rows(const void* x, int64_t M, int32_t K, int64_t ldx, rs_dtype dtype, int8_t* q, int64_t ldq, float* scale,
+                           void* hip_stream) {
+    RS_REQUIRE(dtype == RS_F32 || dtype == RS_BF16, RS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    RS_REQUIRE(M >= 0 && M < ((int64_t)1 << 31), RS_ERR_INVALID_ARG, "M out of range");
+    RS_REQUIRE(K > 0, RS_ERR_INVALID_ARG, "K must be positive");
+    RS_REQUIRE(K <= kGemmI8MaxK, RS_ERR_UNSUPPORTED, "K > %d", kGemmI8MaxK);
+    RS_REQUIRE(ldx >= K && ldq >= K && ldq % 16 == 0, RS_ERR_INVALID_ARG, "ldx and ldq must be at least K, ldq a multiple of 16");
+    RS_REQUIRE(ldx <= kMaxPitch && ldq <= kMaxPitch, RS_ERR_UNSUPPORTED, "ldx or ldq > %lld", (long long)kMaxPitch);
+    if (M == 0) return RS_OK;
+    RS_REQUIRE(x && q && scale, RS_ERR_INVALID_ARG, "x, q and scale must not be NULL");
+    RS_REQUIRE(aligned16(x) && aligned16(q) && aligned4(scale), RS_ERR_INVALID_ARG, "x and q must be 16-byte, scale 4-byte aligned");
+    const size_t es = elem_size(dtype), xb = span(M, ldx, K) * es, qb = span(M, ldq, align_up((size_t)K, 16));
+    RS_REQUIRE(!overlaps(x, xb, q, qb) && !overlaps(x, xb, scale, (size_t)M * 4) && !overlaps(q, qb, scale, (size_t)M * 4),
+               RS_ERR_INVALID_ARG, "x, q and scale must not overlap");
+    hipStream_t st = (hipStream_t)hip_stream;
+    RS_LAUNCH_K(K_LINEAR, st, launch_quantize_rows(dtype, x, ldx, q, ldq, scale, M, K, st));
+    return RS_OK;
+}
+
+static rs_status check_i8_sizes(int32_t K, int32_t N) {
+    RS_REQUIRE(K > 0 && N > 0, RS_ERR_INVALID_ARG, "K and N must be positive");
+    RS_REQUIRE(K <= kGemmI8MaxK && N <= kGemmMaxN, RS_ERR_UNSUPPORTED, "K > %d or N > %d", kGemmI8MaxK, kGemmMaxN);
+    return RS_OK;
+}
+
+rs_status rs_quantize_columns(const void* w, int32_t K, int32_t N, rs_dtype dtype, int8_t* q, float* scale, void* hip_stream) {
+    RS_REQUIRE(dtype == RS_F32 || dtype == RS_BF16, RS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    const rs_status ok = check_i8_sizes(K, N);
+    if (ok != RS_OK) return ok;
+    RS_REQUIRE(w && q && scale, RS_ERR_INVALID_ARG, "w, q and scale must not be NULL");
+    RS_REQUIRE(aligned16(w) && aligned16(q) && aligned4(scale), RS_ERR_INVALID_ARG, "w and q must be 16-byte, scale 4-byte aligned");
+    const size_t n = (size_t)K * N, wb = n * elem_size(dtype);
+    RS_REQUIRE(!overlaps(w, wb, q, n) && !overlaps(w, wb, scale, (size_t)N * 4) && !overlaps(q, n, scale, (size_t)N * 4),
+               RS_ERR_INVALID_ARG, "w, q and scale must not overlap");
+    hipStream_t st = (hipStream_t)hip_stream;
+    RS_LAUNCH_K(K_PACK, st, launch_quantize_columns(dtype, w, q, scale, K, N, st));
+    return RS_OK;
+}
+
+size_t rs_packed_linear_i8_size(int32_t K, int32_t N) { return check_i8_sizes(K, N) == RS_OK ? packed_i8_size(K, N) : 0; }
+
+rs_status rs_pack_linear_i8(const int8_t* q, void* packed, int32_t K, int32_t N, void* hip_stream) {
+    const rs_status ok = check_i8_sizes(K, N);
+    if (ok != RS_OK) return ok;
+    RS_REQUIRE(q && packed, RS_ERR_INVALID_ARG, "q and packed must not be NULL");
+    RS_REQUIRE(aligned16(q) && aligned16(packed), RS_ERR_INVALID_ARG, "q and packed must be 16-byte aligned");
+    RS_REQUIRE(!overlaps(q, (size_t)K * N, packed, packed_i8_size(K, N)), RS_ERR_INVALID_ARG, "packed must not overlap q");
+    hipStream_t st = (hipStream_t)hip_stream;
+    RS_LAUNCH_K(K_PACK, st, launch_pack_i8(q, packed, K, N, st));
+    return RS_OK;
+}
+
+rs_status rs_linear_i8_fwd(const int8_t* a, int64_t lda, const float* a_scale, const void* w, const float* w_scale, const void* bias,
+                           const void* res, void* out, int64_t M, int32_t N, int32_t K, rs_epilogue epi, rs_dtype dtype,
+                           void* hip_stream) {
+    RS_REQUIRE(dtype == RS_F32 || dtype == RS_BF16, RS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    RS_REQUIRE(epi == RS_EPI_BIAS || epi == RS_EPI_BIAS_GELU || epi == RS_EPI_BIAS_RES, RS_ERR_INVALID_ARG,
+               "unknown epilogue %d", (int)epi);
+    RS_REQUIRE(M >= 0 && M < ((int64_t)1 << 31), RS_ERR_INVALID_ARG, "M out of range");
+    const rs_status ok = check_i8_sizes(K, N);
+    if (ok != RS_OK) return ok;
+    RS_REQUIRE(lda >= K && lda % 16 == 0, RS_ERR_INVALID_ARG, "lda must be at least K and a multiple of 16");
+    // a tile's rows are addressed with 32-bit byte offsets from the tile's first row
+    RS_REQUIRE(lda <= kGemmI8MaxPitch, RS_ERR_UNSUPPORTED, "lda > %d", kGemmI8MaxPitch);
+    if (M == 0) return RS_OK;
+    RS_REQUIRE(a && a_scale && w && w_scale && out, RS_ERR_INVALID_ARG, "a, a_scale, w, w_scale and out must not be NULL");
+    RS_REQUIRE(epi != RS_EPI_BIAS_RES || res, RS_ERR_INVALID_ARG, "res must not be NULL for RS_EPI_BIAS_RES");
+    RS_REQUIRE(aligned16(a) && aligned16(w) && aligned16(w_scale) && aligned16(bias) && aligned16(res) && aligned16(out) && aligned4(a_scale),
+               RS_ERR_INVALID_ARG, "tensors must be 16-byte, a_scale 4-byte aligned");
+    const size_t es = elem_size(dtype), ob = (size_t)M * N * es;
+    RS_REQUIRE(!overlaps(out, ob, a, (size_t)M * lda) && !overlaps(out, ob, a_scale, (size_t)M * 4) &&
+                   !overlaps(out, ob, w, packed_i8_size(K, N)) && !overlaps(out, ob, w_scale, (size_t)N * 4) &&
+                   !overlaps(out, ob, bias, N * es) && (epi != RS_EPI_BIAS_RES || res == out || !overlaps(out, ob, res, ob)),
+               RS_ERR_INVALID_ARG, "out must not overlap another tensor (but may be res)");
+    hipStream_t st = (hipStream_t)hip_stream;
+    const GemmEpilogue e = epi == RS_EPI_BIAS ? EPI_BIAS : epi == RS_EPI_BIAS_GELU ? EPI_BIAS_GELU : EPI_BIAS_RES;
+    const GemmI8Args g{a, lda, a_scale, w, w_scale, bias, epi == RS_EPI_BIAS_RES ? res : nullptr, out, M, N, K};
+    RS_LAUNCH_K(K_LINEAR, st, launch_gemm_i8(dtype, e, g, st));
+    return RS_OK;
+}
+
+// ---- norms around the residual add ----------------------------------------------
+rs_status rs_residual_norm_fwd(const rs_residual_norm_cfg* cfg, const rs_residual_norm_weights* w, const void* x, const void* f,
+                               void* y, void* u, int8_t* u_q, int64_t ldq, float* u_scale, void* hip_stream) {
+    RS_REQUIRE(cfg && w, RS_ERR_INVALID_ARG, "cfg and weights must not be NULL");
+    const rs_residual_norm_cfg& c = *cfg;
+    RS_REQUIRE(c.dtype == RS_F32 || c.dtype == RS_BF16, RS_ERR_INVALID_ARG, "unknown dtype %d", (int)c.dtype);
+    RS_REQUIRE(c.post >= RS_NORM_NONE && c.post <= RS_NORM_RMS && c.pre >= RS_NORM_NONE && c.pre <= RS_NORM_RMS, RS_ERR_INVALID_ARG,
+               "unknown norm %d or %d", (int)c.post, (int)c.pre);
+    RS_REQUIRE(c.B >= 0 && c.N >= 0 && c.D > 0, RS_ERR_INVALID_ARG, "B and N must not be negative, D must be positive");
+    RS_REQUIRE(c.D % 8 == 0 && c.D <= kResidualNormMaxD, RS_ERR_UNSUPPORTED, "D must be a multiple of 8 and at most %d", kResidualNormMaxD);
+    RS_REQUIRE((int64_t)c.B * c.N < ((int64_t)1 << 31), RS_ERR_UNSUPPORTED, "B * N >= 2^31");
+    RS_REQUIRE((c.post == RS_NORM_NONE || c.post_eps > 0.f) && (c.pre == RS_NORM_NONE || c.pre_eps > 0.f), RS_ERR_INVALID_ARG,
+               "the eps of a norm must be positive");
+    RS_REQUIRE(c.gate_stride >= 0 && c.mod_stride >= 0 && c.gate_stride % 8 == 0 && c.mod_stride % 8 == 0, RS_ERR_INVALID_ARG,
+               "gate_stride and mod_stride must be multiples of 8 and not negative");
+    RS_REQUIRE(c.gate_stride <= kMaxPitch && c.mod_stride <= kMaxPitch, RS_ERR_UNSUPPORTED, "gate_stride or mod_stride > %lld", (long long)kMaxPitch);
+    RS_REQUIRE((c.post != RS_NORM_NONE || (!w->post_g && !w->post_b)) && (c.pre != RS_NORM_NONE || (!w->pre_g && !w->pre_b)),
+               RS_ERR_INVALID_ARG, "the vectors of a norm that is not taken must be NULL");
+    RS_REQUIRE(f || (c.post == RS_NORM_NONE && !w->gate), RS_ERR_INVALID_ARG, "post must be RS_NORM_NONE and gate NULL if f is NULL");
+    RS_REQUIRE((u_q != nullptr) == (u_scale != nullptr), RS_ERR_INVALID_ARG, "u_q and u_scale: both or neither");
+    RS_REQUIRE(y || u || u_q, RS_ERR_INVALID_ARG, "one of y, u and u_q is wanted");
+    RS_REQUIRE(!u_q || (ldq >= c.D && ldq % 16 == 0), RS_ERR_INVALID_ARG, "ldq must be at least D and a multiple of 16");
+    RS_REQUIRE(!u_q || ldq <= kMaxPitch, RS_ERR_UNSUPPORTED, "ldq > %lld", (long long)kMaxPitch);
+    const int64_t rows = (int64_t)c.B * c.N;
+    if (rows == 0) return RS_OK;
+    RS_REQUIRE(x, RS_ERR_INVALID_ARG, "x is NULL");
+    const void* all[] = {x, f, y, u, u_q, w->post_g, w->post_b, w->gate, w->pre_g, w->pre_b, w->mod_scale, w->mod_shift};
+    for (const void* p : all) RS_REQUIRE(aligned16(p), RS_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+    RS_REQUIRE(aligned4(u_scale), RS_ERR_INVALID_ARG, "u_scale must be 4-byte aligned");
+    const size_t es = elem_size(c.dtype), rb = (size_t)rows * c.D * es, vb = c.D * es;
+    const size_t gb = span(c.B, c.gate_stride * es, vb), mb = span(c.B, c.mod_stride * es, vb);
+    const struct { const void* p; size_t n; } in[] = {{x, rb}, {f, rb}, {w->post_g, vb}, {w->post_b, vb}, {w->gate, gb},
+                                                      {w->pre_g, vb}, {w->pre_b, vb}, {w->mod_scale, mb}, {w->mod_shift, mb}};
+    const struct { const void* p; size_t n; const void* may; } outs[] = {
+        {y, rb, x}, {u, rb, f}, {u_q, span(rows, ldq, align_up((size_t)c.D, 16)), nullptr}, {u_scale, (size_t)rows * 4, nullptr}};
+    for (const auto& o : outs)
+        for (const auto& i : in)
+            RS_REQUIRE((i.p && i.p == o.may && o.p == i.p) || !overlaps(o.p, o.n, i.p, i.n), RS_ERR_INVALID_ARG,
+                       "an output overlaps an input (y may be x, u may be f)");
+    for (const auto& o : outs)
+        for (const auto& q : outs)
+            RS_REQUIRE(&o == &q || !overlaps(o.p, o.n, q.p, q.n), RS_ERR_INVALID_ARG, "outputs overlap each other");
+    hipStream_t st = (hipStream_t)hip_stream;
+    const ResidualNormArgs p{x, f, w->post_g, w->post_b, w->gate, w->pre_g, w->pre_b, w->mod_scale, w->mod_shift, y, u, u_q, u_scale,
+                             rows, c.gate_stride, c.mod_stride, ldq, c.N, c.D, c.post, c.pre, c.post_eps, c.pre_eps, c.x_scale, c.f_scale};
+    RS_LAUNCH_K(K_LN, st, launch_residual_norm(c.dtype, p, st));
+    return RS_OK;
+}
+
 size_t rs_block_workspace_size(const rs_block_cfg* cfg) {
     if (check_cfg(cfg) != RS_OK) return 0;
     return block_layout(cfg).total;
