@@ -164,7 +164,10 @@ def _ptr(t):
 
 def _stream(stream=None):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        if not torch.cuda.is_initialized():
+            return None                  # nobody has chosen a stream yet: the default one
+        # the handle alone: 0.3 us, through torch.cuda.current_stream() 3.4 of the 9.4 that a small call took
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -295,7 +298,7 @@ def _here(*tensors):
     """All on the current device, whose current stream the call goes to."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        assert t is None or (t.is_cuda and t.device.index == dev), "every tensor must be on the current device"
+        assert t is None or t.get_device() == dev, "every tensor must be on the current device"
 
 
 def rs_quantize_rows(x, q, scale, stream=None) -> None:
