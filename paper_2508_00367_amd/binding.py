@@ -7,6 +7,7 @@ library is missing or fails to load, importing the calls raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -328,6 +329,7 @@ def rs_quantize_columns(w, q, scale, stream=None) -> None:
     _check(lib().rs_quantize_columns(_ptr(w), K, N, dtype_code(w.dtype), _ptr(q), _ptr(scale), _stream(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def rs_packed_linear_i8_size(K, N) -> int:
     return int(lib().rs_packed_linear_i8_size(K, N))
 

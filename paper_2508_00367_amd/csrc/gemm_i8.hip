@@ -4,6 +4,9 @@
 // Weights are packed in fragment order, [Np / 32][Kp / 32] fragments of 32 features x 32 k, 1 KB each, lane l's 16 bytes in
 // a row: feature l & 31, k 16 (l >> 5) .. + 15; Np and Kp are N and K rounded up to 64 and 128, the rest is zeros.  A byte of
 // `a` behind column K (up to the row's pitch, or of the next row) is multiplied by such a zero: being an integer it adds nothing.
+#include <type_traits>
+
+#include "gemm_i8_choice.hpp"
 #include "gemm_tile.hpp"
 
 namespace rs {
@@ -171,16 +174,16 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const Ep
 }
 
 // ---------------------------------------------------------------------------
-// Direct kernel: workgroup tile 128 rows x 256 features, four waves of 128 x 64, two workgroups per CU.  Weights go from memory
+// Direct kernel: workgroup tile 32 TM rows x 256 features, four waves of 32 TM x 64, two workgroups per CU.  Weights go from memory
 // straight into the registers of the one wave that needs them, the activations through a ring of four LDS stages of 128 k, copied
 // three slices ahead, as in gemm_bf16_direct_kernel, whose slices hold as many bytes.
 // ---------------------------------------------------------------------------
-template <typename T, int EPI, bool RAGGED>
+template <typename T, int EPI, bool RAGGED, int TM>
 __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale,
                                                                 const int8_t* __restrict__ w, const float* __restrict__ w_scale,
                                                                 const T* __restrict__ bias, const T* res, T* out, int64_t M, int N, int K,
                                                                 int tiles_m, int tiles_n, int gm) {
-    constexpr int TM = 4, TN = 2, BM = 128, BN = 256, RB = 128, STAGE = BM * RB;
+    constexpr int TN = 2, BM = 32 * TM, BN = 256, RB = 128, STAGE = BM * RB;
     __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE];
     __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGE];
     __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGE];
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
     {                                                                                                     \
         const bool real_ = (t_) < S;                                                                      \
         const int kb_ = (t_) * RB;                                                                        \
-        _Pragma("unroll") for (int i = 0; i < 4; ++i)                                                     \
+        _Pragma("unroll") for (int i = 0; i < TM; ++i)                                                    \
             dma16(rs_a, (stage_) + (i * 4 + wave) * 1024, voff, real_ ? i * pass_bytes + kb_ : kPastEnd); \
     }
 // weights of K step kk_ of slice t_
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
         _Pragma("unroll") for (int s_ = 0; s_ < TM; ++s_) {                                               \
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                            \
             __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);                                           \
-            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);                                            \
+            __builtin_amdgcn_sched_group_barrier(0x020, 4 / TM, 0);                                       \
         }                                                                                                 \
         __builtin_amdgcn_sched_barrier(0);                                                                \
     }
@@ -283,7 +286,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
         RS_I8_MFMA(f0, 2)                                                                                 \
         RS_I8_INTERLEAVE()                                                                                \
         RS_I8_W(2, (t_) + 1)                                                                              \
-        RS_I8_WAIT(14)                                                                                    \
+        RS_I8_WAIT(2 * TM + 6)                                                                                    \
         RS_I8_FRAGS(f0, nxt_, 0)                                                                          \
         RS_I8_MFMA(f1, 3)                                                                                 \
         RS_I8_INTERLEAVE()                                                                                \
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
     RS_I8_DMA(st1, 1)
     RS_I8_DMA(st2, 2)
     i8_request_vecs<T, BM, BN>(s_vec, a_scale + m0, w_scale, bias, rows, N, n0, wave, lane);
-    RS_I8_WAIT(16)  // slice 0 has landed: behind it at least 8 weight loads and two slices' copies
+    RS_I8_WAIT(2 * TM + 8)  // slice 0 has landed: behind it at least 8 weight loads and two slices' copies
     RS_I8_FRAGS(f0, st0, 0)
     const int full = S & ~3, left = S & 3;
     for (int t = 0; t < full; t += 4) {
@@ -336,11 +339,340 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
     i8_epilogue<T, EPI, TM, RAGGED>(acc, reg, s_vec, res, out, M, N, m0, n_base, 0, wave * 64, lane);
 }
 
+// ---------------------------------------------------------------------------
+// Split kernel, for the smallest problems: 32 rows x 32 TN features, the slices of K dealt out to the eight waves, two of them at a
+// time in registers straight from memory, the partial sums added in LDS by integer atomics, whose order does not matter.
+// What bounds such a call is the way to memory and back, once or twice, not bytes: no barrier before the sums meet, everything
+// the epilogue reads requested behind the first slices.  (Slices past K requested and multiplied as zeros, without the peeled
+// tail: 1 x 768 -> 2304 3.4 -> 4.1 us.)
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void ld4(const T* p, int n, bool vec, float (&v)[4]) {  // n of 4 values
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 r = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = r[e];
+        } else {
+            const uint2 r = *reinterpret_cast<const uint2*>(p);
+            v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
+            v[2] = __uint_as_float(r.y << 16); v[3] = __uint_as_float(r.y & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < n ? Elem<T>::ld(p + e) : 0.f;
+    }
+}
+
+template <typename T, int EPI, int TN>
+__global__ __launch_bounds__(512, TN > 1 ? 2 : 4) void gemm_i8_split_kernel(
+    const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale, const int8_t* __restrict__ w,
+    const float* __restrict__ w_scale, const T* __restrict__ bias, const T* res, T* out, int64_t M, int N, int K, int tiles_n) {
+    constexpr int W = 8, BM = 32, BN = 32 * TN, LD = BN + 1;
+    __shared__ int s_sum[BM * LD];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * BM;
+    const int n0 = (int)(blockIdx.x % tiles_n) * BN;
+    const int S = (K + 127) >> 7, frag_row = S * 4096;
+    const int rows = (int)(M - m0 < BM ? M - m0 : BM);
+    const __amdgpu_buffer_rsrc_t rs_a = make_rsrc(a + m0 * lda, (int64_t)rows * lda);
+    // rows of fragments: Np / 32 of them, an even number
+    const __amdgpu_buffer_rsrc_t rs_w = make_rsrc(w + (int64_t)(n0 >> 5) * frag_row, (int64_t)TN * frag_row);
+    const int aoff = l32 * lda + g * 16, woff = lane * 16;
+
+    i32x4 av[2][4], wv[2][4][TN];
+    i32x16 acc[TN];
+    auto request = [&](int b, int kk, int t) {  // K step kk of slice t
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            wv[b][kk][j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs_w, woff, j * frag_row + t * 4096 + kk * 1024, 0));
+        av[b][kk] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs_a, aoff, t * 128 + kk * 32, 0));
+    };
+    // the products of a slice; more: each step's registers requested again for this wave's slice after next
+    auto slice = [&](int b, int t, auto more) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wv[b][kk][j], av[b][kk], acc[j], 0, 0, 0);
+            if constexpr (decltype(more)::value) {
+                request(b, kk, t + 2 * W);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+        if (wave + b * W < S) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) request(b, kk, wave + b * W);
+        }
+    // Thread t writes features 4 (t % (BN / 4)) .. + 3 of row t / (BN / 4); the first 32 BN / 4 of the 512.
+    constexpr int PER_ROW = BN / 4;
+    const int ec = n0 + (tid % PER_ROW) * 4, er = tid / PER_ROW;
+    const int ne = er < rows ? min(N - ec, 4) : 0;
+    const bool vec = N % 4 == 0;
+    float ws[4] = {0.f, 0.f, 0.f, 0.f}, bv[4] = {0.f, 0.f, 0.f, 0.f}, rv[4] = {0.f, 0.f, 0.f, 0.f}, as = 0.f;
+    if (ne > 0) {
+        ld4(w_scale + ec, ne, ne == 4, ws);
+        if (bias) ld4(bias + ec, ne, ne == 4, bv);
+        as = a_scale[m0 + er];
+        if (EPI == EPI_BIAS_RES) ld4(res + (m0 + er) * N + ec, ne, vec, rv);
+    }
+    for (int i = tid; i < BM * LD; i += 64 * W) s_sum[i] = 0;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][r] = 0;
+    int t = wave;
+    for (; t + 3 * W < S; t += 2 * W) {
+        slice(0, t, std::true_type{});
+        slice(1, t + W, std::true_type{});
+    }
+    if (t + 2 * W < S) {  // three slices left, two of them in registers
+        slice(0, t, std::true_type{});
+        slice(1, t + W, std::false_type{});
+        slice(0, t + 2 * W, std::false_type{});
+    } else {
+        if (t < S) slice(0, t, std::false_type{});
+        if (t + W < S) slice(1, t + W, std::false_type{});
+    }
+    __syncthreads();  // the sums are zero
+    if (wave < S) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) atomicAdd(&s_sum[l32 * LD + j * 32 + (r >> 2) * 8 + g * 4 + (r & 3)], acc[j][r]);
+    }
+    __syncthreads();
+    if (ne <= 0) return;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = fmaf((float)s_sum[er * LD + ec - n0 + e], as * ws[e], bv[e]);
+        if (EPI == EPI_BIAS_GELU) v[e] = gelu_of(v[e], (const T*)nullptr);
+        if (EPI == EPI_BIAS_RES) v[e] += rv[e];
+    }
+    T* o = out + (m0 + er) * N + ec;
+    if (vec) {
+        put4((unsigned char*)o, v, (T*)nullptr);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < ne) Elem<T>::st(o + e, v[e]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Private kernel, for grids in between: 64 rows x 64 features, the slices of K dealt out to four waves, each with two stages of
+// its own for the rows (whole lines by direct copies) and its weights in registers: no barrier before the sums meet.  They
+// do so in LDS, where the first two waves collect the 32-row group that they then write.  Two workgroups per CU.
+// (128 rows, one workgroup per CU: 512 x 4096 -> 4096 15.2 -> 13.9 us, where every CU has one such tile, elsewhere slower: 788 x 768 -> 2304
+// 6.4 -> 6.8, 1576 x 4096 -> 1024 the same.)
+// ---------------------------------------------------------------------------
 template <typename T, int EPI, bool RAGGED>
+__global__ __launch_bounds__(256, 2) void gemm_i8_private_kernel(
+    const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale, const int8_t* __restrict__ w,
+    const float* __restrict__ w_scale, const T* __restrict__ bias, const T* res, T* out, int64_t M, int N, int K, int tiles_m,
+    int tiles_n, int gm) {
+    constexpr int W = 4, TM = 2, TN = 2, BM = 32 * TM, BN = 64, RB = 128, STAGE = BM * RB;
+    __shared__ __attribute__((aligned(1024))) unsigned char st0[W * STAGE];
+    __shared__ __attribute__((aligned(1024))) unsigned char st1[W * STAGE];
+    __shared__ __attribute__((aligned(1024))) unsigned char s_vec[kVecBytes];
+    int64_t m0;
+    int n0;
+    {
+        const int nblk = tiles_m * tiles_n;
+        const int xcd = blockIdx.x & 7;
+        const int xq = nblk >> 3, xr = nblk & 7;
+        const int x_cnt = xq + (xcd < xr ? 1 : 0), x_start = xcd * xq + (xcd < xr ? xcd : xr);
+        const int seq = blockIdx.x >> 3;
+        if (seq >= x_cnt) return;  // whole workgroup, before any barrier
+        const int bid = x_start + seq;
+        const int per_group = gm * tiles_n;
+        const int grp = bid / per_group, rem = bid - grp * per_group;
+        const int first_m = grp * gm;
+        const int gsz = min(tiles_m - first_m, gm);
+        const int tn = rem / gsz;
+        n0 = tn * BN;
+        m0 = (int64_t)(first_m + rem - tn * gsz) * BM;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int S = (K + 127) >> 7, frag_row = S * 4096;
+    const int64_t rows = M - m0 < BM ? M - m0 : BM;
+    const __amdgpu_buffer_rsrc_t rs_a = make_rsrc(a + m0 * lda, rows * lda);
+    const __amdgpu_buffer_rsrc_t rs_w = make_rsrc(w + (int64_t)(n0 >> 5) * frag_row, 2 * frag_row);
+    const int ld_r = lane >> 3, ld_p = lane & 7;
+    // copy i takes rows 8 i .. + 7; chunk c of row r in slot c ^ (r & 7) ^ ((r >> 3) & 1)
+    const int voff0 = ld_r * lda + ((ld_p ^ ld_r) << 4), voff1 = (8 + ld_r) * lda + ((ld_p ^ ld_r ^ 1) << 4);
+    const int sw = (l32 & 7) ^ ((l32 >> 3) & 1);
+    const int woff0 = lane * 16, woff1 = woff0 + frag_row;
+    const int mine = wave * STAGE;
+
+    i32x4 wf[2][4][TN], f0[TM], f1[TM];
+    i32x16 acc[TN][TM];
+#define RS_I8_ROWS(stage_, t_)                                                                            \
+    {                                                                                                     \
+        const int kb_ = (t_) * RB;                                                                        \
+        _Pragma("unroll") for (int i = 0; i < BM / 16; ++i) {                                             \
+            dma16(rs_a, (stage_) + mine + i * 2048, voff0, i * 16 * lda + kb_);                           \
+            dma16(rs_a, (stage_) + mine + i * 2048 + 1024, voff1, i * 16 * lda + kb_);                    \
+        }                                                                                                 \
+    }
+#define RS_I8_W(b_, t_)                                                                                   \
+    {                                                                                                     \
+        _Pragma("unroll") for (int kk = 0; kk < 4; ++kk) {                                                \
+            const int so_ = ((t_) * 4 + kk) * 1024;                                                       \
+            wf[b_][kk][0] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs_w, woff0, so_, 0)); \
+            wf[b_][kk][1] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs_w, woff1, so_, 0)); \
+        }                                                                                                 \
+    }
+#define RS_I8_FRAGS(f_, stage_, kk_)                                                                      \
+    {                                                                                                     \
+        const int co_ = ((((kk_) * 2 + g) ^ sw) << 4);                                                    \
+        _Pragma("unroll") for (int j = 0; j < TM; ++j)                                                    \
+            f_[j] = *reinterpret_cast<const i32x4*>((stage_) + mine + (l32 + j * 32) * RB + co_);         \
+    }
+#define RS_I8_MFMA(f_, b_, kk_)                                                                           \
+    {                                                                                                     \
+        _Pragma("unroll") for (int i = 0; i < TN; ++i)                                                    \
+            _Pragma("unroll") for (int j = 0; j < TM; ++j)                                                \
+                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[b_][kk_][i], f_[j], acc[i][j], 0, 0, 0); \
+    }
+// A slice from stage_ and wf[b_]; what it has been waited for is the caller's
+#define RS_I8_COMPUTE(stage_, b_)                                                                         \
+    {                                                                                                     \
+        RS_I8_FRAGS(f0, stage_, 0)                                                                        \
+        RS_I8_FRAGS(f1, stage_, 1)                                                                        \
+        RS_I8_MFMA(f0, b_, 0)                                                                             \
+        RS_I8_FRAGS(f0, stage_, 2)                                                                        \
+        RS_I8_MFMA(f1, b_, 1)                                                                             \
+        RS_I8_FRAGS(f1, stage_, 3)                                                                        \
+        RS_I8_MFMA(f0, b_, 2)                                                                             \
+        RS_I8_MFMA(f1, b_, 3)                                                                             \
+    }
+    constexpr int SLICE_LOADS = BM / 8 + 8;
+#define RS_I8_WAIT(n_)                                                                                    \
+    {                                                                                                     \
+        __builtin_amdgcn_s_waitcnt(((n_) & 15) | (((n_) >> 4) << 14) | 0x0070); /* and every LDS read */  \
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");                                            \
+        __builtin_amdgcn_sched_barrier(0);                                                                \
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    i8_request_vecs<T, BM, BN>(s_vec, a_scale + m0, w_scale, bias, rows, N, n0, wave, lane);
+    if (wave < S) {
+        RS_I8_ROWS(st0, wave)
+        RS_I8_W(0, wave)
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    int t = wave;
+    for (; t + 2 * W < S; t += 2 * W) {  // a stage is free once its slice has been read: the next but one goes there
+        RS_I8_ROWS(st1, t + W)
+        RS_I8_W(1, t + W)
+        RS_I8_WAIT(SLICE_LOADS)
+        RS_I8_COMPUTE(st0, 0)
+        RS_I8_WAIT(SLICE_LOADS)
+        RS_I8_ROWS(st0, t + 2 * W)
+        RS_I8_W(0, t + 2 * W)
+        RS_I8_WAIT(SLICE_LOADS)
+        RS_I8_COMPUTE(st1, 1)
+        RS_I8_WAIT(SLICE_LOADS)
+    }
+    if (t + W < S) {
+        RS_I8_ROWS(st1, t + W)
+        RS_I8_W(1, t + W)
+        RS_I8_WAIT(SLICE_LOADS)
+        RS_I8_COMPUTE(st0, 0)
+        RS_I8_WAIT(0)
+        RS_I8_COMPUTE(st1, 1)
+    } else if (t < S) {
+        RS_I8_WAIT(0)
+        RS_I8_COMPUTE(st0, 0)
+    }
+#undef RS_I8_ROWS
+#undef RS_I8_W
+#undef RS_I8_FRAGS
+#undef RS_I8_MFMA
+#undef RS_I8_COMPUTE
+#undef RS_I8_WAIT
+    // Group j of the tile goes to wave j: the others leave theirs in slots of 8 KB, [group][other wave], 16 bytes per lane.
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & 0xC07F);  // the vectors have landed
+    __syncthreads();  // every wave has read its stages
+    constexpr int PER = W * STAGE / 8192;  // slots of a stage array
+    static_assert(TM * (W - 1) <= 2 * PER, "slots");
+    auto slot = [&](int j, int from) {
+        const int at = j * (W - 1) + from;
+        return (at < PER ? st0 + at * 8192 : st1 + (at - PER) * 8192) + lane * 16;
+    };
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+        if (j != wave) {
+            unsigned char* s = slot(j, wave - (wave > j ? 1 : 0));
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<i32x4*>(s + (i * 4 + q) * 1024) = i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        }
+    __syncthreads();
+    if (wave >= TM) return;
+    i32x16 sum[TN][1];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) sum[i][0] = wave == 0 ? acc[i][0] : acc[i][1];
+#pragma unroll
+    for (int o = 0; o < W - 1; ++o) {
+        const unsigned char* s = slot(wave, o);
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const i32x4 v = *reinterpret_cast<const i32x4*>(s + (i * 4 + q) * 1024);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[i][0][4 * q + e] += v[e];
+            }
+    }
+    EpiRegions<1> reg;
+    reg.r[0] = slot(wave, 0) - lane * 16;  // read by this wave alone, and it has been read
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    i8_epilogue<T, EPI, 1, RAGGED>(sum, reg, s_vec, res, out, M, N, m0 + wave * 32, n0, wave * 32, 0, lane);
+}
+
+template <typename T, int EPI, bool RAGGED, int TM>
 static void launch_i8_direct(const GemmI8Args& g, hipStream_t s) {
-    const int tiles_m = (int)((g.M + 127) / 128), tiles_n = (g.N + 255) / 256, nblk = tiles_m * tiles_n;
-    hipLaunchKernelGGL((gemm_i8_direct_kernel<T, EPI, RAGGED>), dim3(8 * ((nblk + 7) / 8)), dim3(256), 0, s, g.a, (int)g.lda, g.a_scale,
+    const int tiles_m = (int)((g.M + 32 * TM - 1) / (32 * TM)), tiles_n = (g.N + 255) / 256, nblk = tiles_m * tiles_n;
+    hipLaunchKernelGGL((gemm_i8_direct_kernel<T, EPI, RAGGED, TM>), dim3(8 * ((nblk + 7) / 8)), dim3(256), 0, s, g.a, (int)g.lda, g.a_scale,
                        (const int8_t*)g.w, g.w_scale, (const T*)g.bias, (const T*)g.res, (T*)g.out, g.M, g.N, g.K, tiles_m, tiles_n, 16);
+}
+
+template <typename T, int EPI, bool RAGGED>
+static void launch_i8_private(const GemmI8Args& g, hipStream_t s) {
+    const int tiles_m = (int)((g.M + 63) / 64), tiles_n = (g.N + 63) / 64, nblk = tiles_m * tiles_n;
+    hipLaunchKernelGGL((gemm_i8_private_kernel<T, EPI, RAGGED>), dim3(8 * ((nblk + 7) / 8)), dim3(256), 0, s, g.a, (int)g.lda, g.a_scale,
+                       (const int8_t*)g.w, g.w_scale, (const T*)g.bias, (const T*)g.res, (T*)g.out, g.M, g.N, g.K, tiles_m, tiles_n, 16);
+}
+
+template <typename T, int EPI, int TN>
+static void launch_i8_split(const GemmI8Args& g, hipStream_t s) {
+    const int tiles_n = (g.N + 32 * TN - 1) / (32 * TN), tiles = (int)((g.M + 31) / 32 * tiles_n);
+    hipLaunchKernelGGL((gemm_i8_split_kernel<T, EPI, TN>), dim3(tiles), dim3(512), 0, s, g.a, (int)g.lda, g.a_scale, (const int8_t*)g.w,
+                       g.w_scale, (const T*)g.bias, (const T*)g.res, (T*)g.out, g.M, g.N, g.K, tiles_n);
+}
+
+template <typename T, int EPI, bool RAGGED>
+static void launch_i8_part(const GemmI8Args& g, hipStream_t s) {
+    switch (gemm_i8_choose(g.M, g.N, g.K, device_cus())) {
+        case GemmI8Tile::Split32x32: launch_i8_split<T, EPI, 1>(g, s); break;
+        case GemmI8Tile::Split32x64: launch_i8_split<T, EPI, 2>(g, s); break;
+        case GemmI8Tile::Private64x64: launch_i8_private<T, EPI, RAGGED>(g, s); break;
+        case GemmI8Tile::Direct64x256: launch_i8_direct<T, EPI, RAGGED, 2>(g, s); break;
+        case GemmI8Tile::Direct128x256: launch_i8_direct<T, EPI, RAGGED, 4>(g, s); break;
+    }
 }
 
 // Rows in parts of at most 2^22 tiles of 128 x 64 (a launch holds fewer than 2^32 threads).
@@ -354,8 +686,8 @@ static hipError_t launch_i8(const GemmI8Args& g, hipStream_t s) {
         p.res = g.res ? (const T*)g.res + r * g.N : nullptr;
         p.out = (T*)g.out + r * g.N;
         p.M = g.M - r < rows ? g.M - r : rows;
-        if ((int64_t)g.N * sizeof(T) % 16) launch_i8_direct<T, EPI, true>(p, s);
-        else launch_i8_direct<T, EPI, false>(p, s);
+        if ((int64_t)g.N * sizeof(T) % 16) launch_i8_part<T, EPI, true>(p, s);
+        else launch_i8_part<T, EPI, false>(p, s);
     }
     return hipGetLastError();
 }

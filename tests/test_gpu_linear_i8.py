@@ -78,6 +78,36 @@ def test_linear_i8(M, K, N, epi, dtype):
     check(run_linear(*t, dtype, epi), *t, dtype, epi)
 
 
+# One size for each kernel, rows of whole 16-byte pieces and others: tests/test_i8_choice_cpu.py has which is which.
+EVERY_KERNEL = [(40, 300, 200), (197, 768, 2304), (197, 770, 1155), (788, 768, 768), (900, 200, 1001), (788, 4096, 1024), (1576, 768, 2304),
+                (1700, 1300, 2051), (1576, 1024, 4096), (2500, 1100, 3001)]
+
+
+@pytest.mark.parametrize("epi,dtype", [("bias", "bf16"), ("gelu", "bf16"), ("res", "bf16"), ("res", "f32"), ("gelu", "f32")])
+@pytest.mark.parametrize("M,K,N", EVERY_KERNEL)
+def test_every_kernel(M, K, N, epi, dtype):
+    """Against 64 bits in the outer rows and columns and a sample of the others, where a tile's edges are."""
+    _say("every kernel", M, K, N, epi, dtype)
+    a, a_s, w, w_s, bias, res = make(M, K, N, dtype, epi, seed=M + N)
+    out = run_linear(a, a_s, w, w_s, bias, res, dtype, epi)
+    rows = sorted(set(range(70)) | set(range(M - 140, M)) | set(range(0, M, 37))) if M > 400 else list(range(M))
+    check(out[rows], a[rows], a_s[rows], w, w_s, bias, None if res is None else res[rows], dtype, epi)
+    cols = sorted(set(range(min(N, 70))) | set(range(max(N - 70, 0), N)))
+    check(out[:, cols], a, a_s, w[:, cols], w_s[cols], bias[cols], None if res is None else res[:, cols], dtype, epi)
+
+
+@pytest.mark.parametrize("K", [1, 127, 128, 129, 640, 1024, 1025, 2048, 3200, 5000, 9000])
+@pytest.mark.parametrize("M,N", [(33, 70), (300, 1100), (1100, 3000)])
+def test_every_length_of_the_inner_axis(M, N, K):
+    """Rings and peeled tails of every kernel, from one slice to many; exact sums, so every row is the same where the rows are."""
+    _say("inner axis", M, K, N)
+    a, a_s, w, w_s, bias, _ = make(M, K, N, "f32", "bias", seed=K)
+    a[1:], a_s[1:] = a[:1].clone(), a_s[:1].clone()
+    out = run_linear(a, a_s, w, w_s, bias, None, "f32", "bias")
+    check(out[:1], a[:1], a_s[:1], w, w_s, bias, None, "f32", "bias")
+    assert bool((out == out[:1]).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_bias_no_rows_and_out_is_res(dtype):
     a, a_s, w, w_s, bias, res = make(70, 96, 136, dtype, "res", 5)
