@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNormArgs p) 
     const int t = threadIdx.x & (64 * WPR - 1), D = p.D, nchunk = D >> 3;
     const T *xp = (const T*)p.x, *fp = (const T*)p.f, *post_g = (const T*)p.post_g, *post_b = (const T*)p.post_b;
     const T *pre_g = (const T*)p.pre_g, *pre_b = (const T*)p.pre_b;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / (64 * WPR); row < p.rows; row += (int64_t)gridDim.x * RPB) {
+    for (int64_t row = (int64_t)blockIdx.x * RPB + (WPR == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0); row < p.rows; row += (int64_t)gridDim.x * RPB) {
         const int64_t img = row / p.N;
         const T* gate = p.gate ? (const T*)p.gate + img * p.gate_stride : nullptr;
         const T* ms = p.mod_scale ? (const T*)p.mod_scale + img * p.mod_stride : nullptr;
@@ -143,12 +143,22 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNormArgs p) 
     }
 }
 
+template <typename T, int MAXC, int WPR>
+static hipError_t go(const ResidualNormArgs& p, hipStream_t s) {
+    constexpr int RPB = 4 / WPR;
+    const int64_t blocks = (p.rows + RPB - 1) / RPB;
+    hipLaunchKernelGGL((residual_norm_kernel<T, MAXC, WPR>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
 template <typename T>
 static hipError_t launch_rn(const ResidualNormArgs& p, hipStream_t s) {
-    const dim3 grid((unsigned)(p.rows < 1 << 20 ? p.rows : 1 << 20));
-    if (p.D <= 2048) hipLaunchKernelGGL((residual_norm_kernel<T, 1, 4>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((residual_norm_kernel<T, 8, 4>), grid, dim3(256), 0, s, p);
-    return hipGetLastError();
+    if (p.D <= 512) return go<T, 1, 1>(p, s);
+    if (p.D <= 1024) return go<T, 2, 1>(p, s);
+    if (p.D <= 2048) return go<T, 4, 1>(p, s);
+    if (p.D <= 4096) return go<T, 2, 4>(p, s);
+    if (p.D <= 8192) return go<T, 4, 4>(p, s);
+    return go<T, 8, 4>(p, s);
 }
 
 hipError_t launch_residual_norm(rs_dtype dt, const ResidualNormArgs& p, hipStream_t s) {
