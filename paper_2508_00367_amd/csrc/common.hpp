@@ -362,6 +362,7 @@ struct ResidualNormArgs {
     float post_eps, pre_eps, x_scale, f_scale;
 };
 constexpr int kResidualNormMaxD = 16384;
+constexpr int kResidualNormMaxStride = 1 << 24;  // of an image's vectors: a wave reaches over up to 8 images with 32-bit byte offsets
 hipError_t launch_residual_norm(rs_dtype dt, const ResidualNormArgs& p, hipStream_t s);
 
 // bf16 [K, N] row-major -> [N, K] row-major

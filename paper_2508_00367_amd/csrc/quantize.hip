@@ -7,8 +7,8 @@
 
 namespace rs {
 
-// 16 values of a row from column k on, k a multiple of 16; zeros from column K on.  VEC: rows start 16-byte aligned (the
-// resource ends with the last whole word of the row: an odd count of bf16 ends a word early, and is not VEC).
+// 16 values of a row from column k on, k a multiple of 16; zeros from column K on.  VEC: rows are whole 16-byte pieces and start
+// 16-byte aligned, and a resource ends with the row.
 template <typename T, bool VEC>
 __device__ __forceinline__ void load16(__amdgpu_buffer_rsrc_t row, const T* p, int k, int K, float (&v)[16]) {
     if constexpr (VEC) {
@@ -25,6 +25,11 @@ __device__ __forceinline__ void load16(__amdgpu_buffer_rsrc_t row, const T* p, i
                 }
             }
         }
+    } else if (k + 16 <= K) {  // aligned to its elements only (the hardware takes that in its stride)
+        struct __attribute__((packed, aligned(sizeof(T)))) { T e[16]; } raw;
+        __builtin_memcpy(&raw, p + k, sizeof(raw));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = Elem<T>::ld(&raw.e[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = k + i < K ? Elem<T>::ld(p + k + i) : 0.f;
@@ -123,11 +128,13 @@ static void by_width(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* 
         if (K <= 256) RS_Q(16, 1, true, false);
         else if (K <= 512) RS_Q(32, 1, true, false);
         else if (K <= 1024) RS_Q(64, 1, true, false);
+        else if (K <= 2048 && sizeof(T) == 2) RS_Q(64, 2, true, false);
         else if (K <= 4096) RS_Q(256, 1, true, false);
         else if (K <= 16384) RS_Q(256, 4, true, false);
         else RS_Q(256, 1, true, true);
     } else {
         if (K <= 1024) RS_Q(64, 1, false, false);
+        else if (K <= 4096) RS_Q(256, 1, false, false);
         else RS_Q(256, 1, false, true);
     }
 #undef RS_Q

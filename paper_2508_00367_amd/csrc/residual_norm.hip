@@ -7,192 +7,211 @@
 
 namespace rs {
 
-// 8 elements as they are in memory.
-template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };
+// 16 bytes of a row, 8 or 4 channels: what a lane loads and stores at a time, its neighbours the ones beside it.
+template <typename T> constexpr int kE = 16 / (int)sizeof(T);
 
-// `off`: byte offset, or one past the resource's end (zeros).
 template <typename T>
-__device__ __forceinline__ Raw8<T> raw_load(__amdgpu_buffer_rsrc_t r, int off) {
-    Raw8<T> v;
-#pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.w[h] = __builtin_amdgcn_raw_buffer_load_b128(r, off + h * 16, 0, 0);
-    return v;
+__device__ __forceinline__ float at(u32x4 w, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
 }
 template <typename T>
-__device__ __forceinline__ Raw8<T> raw_load(const T* p) {
-    Raw8<T> v;
-#pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.w[h] = reinterpret_cast<const u32x4*>(p)[h];
-    return v;
-}
-template <typename T>
-__device__ __forceinline__ float at(const Raw8<T>& v, int i) {
-    if constexpr (sizeof(T) == 4) return __uint_as_float(v.w[i >> 2][i & 3]);
-    else return __uint_as_float((i & 1) ? (v.w[0][i >> 1] & 0xffff0000u) : (v.w[0][i >> 1] << 16));
+__device__ __forceinline__ u32x4 piece(const float (&v)[kE<T>]) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    else return u32x4{pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7])};
 }
 
-// Sum, or the largest magnitude, over the G lanes of a row (256: the four waves of a workgroup, in wave order).
+// Sum, or the largest magnitude, over the G lanes of a row (more than 64: the waves of a workgroup, in wave order).
 template <int G, bool MAX>
 __device__ __forceinline__ float row_reduce(float v, float* s) {
     auto op = [](float a, float b) { return MAX ? amax_step(a, b) : a + b; };
     v = lanes_reduce<(G < 64 ? G : 64)>(v, op);
-    if constexpr (G == 256) {
+    if constexpr (G > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = op(op(op(s[0], s[1]), s[2]), s[3]);
+        v = s[0];
+#pragma unroll
+        for (int i = 1; i < G / 64; ++i) v = op(v, s[i]);
     }
     return v;
 }
 
-// v = Norm(v); chunks past the row's end hold zeros before and after, and the deviations leave them out.
-template <int G, int MAXC>
-__device__ __forceinline__ void row_norm(float (&v)[MAXC][8], rs_norm kind, float eps, float inv_d, int nchunk, int sub, float* s) {
+// v = Norm(v); pieces past the row's end (`n` of them are inside) hold zeros before and after, and the deviations leave them out.
+template <int G, int P, int E>
+__device__ __forceinline__ void row_norm(float (&v)[P][E], rs_norm kind, float eps, float inv_d, int n, int sub, float* s) {
     if (kind == RS_NORM_NONE) return;
-    float mean = 0.f;
     if (kind == RS_NORM_LAYER) {
         float sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c)
+        for (int c = 0; c < P; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[c][i];
-        mean = row_reduce<G, false>(sum, s) * inv_d;
+            for (int i = 0; i < E; ++i) sum += v[c][i];
+        const float mean = row_reduce<G, false>(sum, s) * inv_d;
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c)
+        for (int c = 0; c < P; ++c) {
+            const float m = sub + c * G < n ? mean : 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = sub + c * G < nchunk ? v[c][i] - mean : 0.f;
+            for (int i = 0; i < E; ++i) v[c][i] -= m;
+        }
     }
     float sq = 0.f;
 #pragma unroll
-    for (int c = 0; c < MAXC; ++c)
+    for (int c = 0; c < P; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fmaf(v[c][i], v[c][i], sq);
+        for (int i = 0; i < E; ++i) sq = fmaf(v[c][i], v[c][i], sq);
     const float r = rsqrtf(fmaf(row_reduce<G, false>(sq, s), inv_d, eps));
 #pragma unroll
-    for (int c = 0; c < MAXC; ++c)
+    for (int c = 0; c < P; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] *= r;
+        for (int i = 0; i < E; ++i) v[c][i] *= r;
 }
 
-// G lanes per row (8 .. 64, or a workgroup of 256), MAXC chunks of 8 channels per lane: lane l has chunks l, l + G, ...
+// G lanes per row (8 .. 64, or a workgroup of 256 .. 1024), P pieces per lane: lane l has pieces l, l + G, ...
 // The rows of a wave are neighbours: one resource holds them, and what lies past the last row or the end of a row is aimed
-// past its end.
-template <typename T, int G, int MAXC>
-__global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNormArgs p) {
-    __shared__ float s_red[4];
-    constexpr int RPW = G < 64 ? 64 / G : 1, RPB = G == 256 ? 1 : 4 * RPW;  // rows of a wave, of a workgroup
-    constexpr int ES = sizeof(T);
-    const int D = p.D, nchunk = D >> 3, sub = threadIdx.x % G;
+// past its end.  Outputs are written through the L2 (store16_wt).
+template <typename T, int G, int P>
+__global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(ResidualNormArgs p) {
+    __shared__ float s_red[G > 64 ? G / 64 : 1];
+    constexpr int RPW = G < 64 ? 64 / G : 1, RPB = G > 64 ? 1 : 4 * RPW;  // rows of a wave, of a workgroup
+    constexpr int ES = sizeof(T), E = kE<T>;
+    const int D = p.D, n = D / E, sub = threadIdx.x % G;
     const float inv_d = 1.0f / (float)D;
-    const bool has_f = p.f != nullptr;
-    const T *post_g = (const T*)p.post_g, *post_b = (const T*)p.post_b, *pre_g = (const T*)p.pre_g, *pre_b = (const T*)p.pre_b;
-    const int64_t wave0 = (int64_t)blockIdx.x * RPB + (G == 256 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPW);
+    const int64_t wave0 = (int64_t)blockIdx.x * RPB + (G > 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPW);
     for (int64_t row0 = wave0; row0 < p.rows; row0 += (int64_t)gridDim.x * RPB) {
         const int my = G < 64 ? (threadIdx.x & 63) / G : 0;
-        const int64_t left = p.rows - row0;
+        const int64_t left = p.rows - row0, row = row0 + my;
+        const bool on = my < left;
         const int bytes = (int)(left < RPW ? left : RPW) * D * ES;
-        const __amdgpu_buffer_rsrc_t rs_x = row_rsrc((const T*)p.x + row0 * D, bytes);
-        const __amdgpu_buffer_rsrc_t rs_f = row_rsrc(has_f ? (const T*)p.f + row0 * D : nullptr, has_f ? bytes : 0);
-        int off[MAXC];
+        auto rsrc = [&](const void* q) { return row_rsrc(q ? (const T*)q + row0 * D : nullptr, q ? bytes : 0); };
+        const __amdgpu_buffer_rsrc_t rs_x = rsrc(p.x), rs_f = rsrc(p.f), rs_y = rsrc(p.y), rs_u = rsrc(p.u);
+        int off[P];
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c) off[c] = sub + c * G < nchunk ? (my * D + (sub + c * G) * 8) * ES : 0x7fffff00;
-        Raw8<T> rx[MAXC], w[MAXC];
-        float v[MAXC][8];
+        for (int c = 0; c < P; ++c) off[c] = sub + c * G < n ? my * D * ES + (sub + c * G) * 16 : 0x7fffff00;
+        u32x4 rx[P], w[P], va[P], vb[P], vc[P], vd[P];
+        float v[P][E];
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c) w[c] = raw_load<T>(rs_f, off[c]);
+        for (int c = 0; c < P; ++c) w[c] = __builtin_amdgcn_raw_buffer_load_b128(rs_f, off[c], 0, 0);
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c) rx[c] = raw_load<T>(rs_x, off[c]);
-        // a vector's chunks of this lane; past the row's end its first one, of which nothing is used
-        auto vec = [&](const T* q) {
-#pragma unroll
-            for (int c = 0; c < MAXC; ++c) w[c] = raw_load<T>(q + (sub + c * G < nchunk ? sub + c * G : 0) * 8);
-        };
-        int64_t img = 0;
+        for (int c = 0; c < P; ++c) rx[c] = __builtin_amdgcn_raw_buffer_load_b128(rs_x, off[c], 0, 0);
+        // Vectors: this lane's pieces (past the row's end the first one, of which nothing is used), the image's by their distance from
+        // those of the wave's first row.
+        int64_t img0 = 0;
+        int at_gate = 0, at_mod = 0;
         if (p.gate_stride | p.mod_stride) {
-            const int64_t row = row0 + my < p.rows ? row0 + my : p.rows - 1;
-            img = (uint32_t)row / (uint32_t)p.N;
+            img0 = (uint32_t)row0 / (uint32_t)p.N;
+            if constexpr (G < 64) {
+                const int d = (int)((uint32_t)(on ? row : p.rows - 1) / (uint32_t)p.N) - (int)img0;
+                at_gate = d * (int)p.gate_stride * ES;
+                at_mod = d * (int)p.mod_stride * ES;
+            }
         }
+        auto vec = [&](auto& r, const void* q, int64_t first, int by) {
+            const __amdgpu_buffer_rsrc_t rs = row_rsrc((const T*)q + first, 0x7fffffff);
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c)
+            for (int c = 0; c < P; ++c) r[c] = __builtin_amdgcn_raw_buffer_load_b128(rs, (sub + c * G < n ? (sub + c * G) * 16 : 0) + by, 0, 0);
+        };
+#define RS_VEC(r_, name_) if (p.name_) vec(r_, p.name_, 0, 0)
+#define RS_VEC_GATE(r_) if (p.gate) vec(r_, p.gate, img0 * p.gate_stride, at_gate)
+#define RS_VEC_MOD(r_, name_) if (p.name_) vec(r_, p.name_, img0 * p.mod_stride, at_mod)
+// each of the lane's values with its place t in a vector
+#define RS_EACH(cond_, r_, expr_)                                                                        \
+    if (cond_) {                                                                                          \
+        _Pragma("unroll") for (int c = 0; c < P; ++c)                                                     \
+            _Pragma("unroll") for (int i = 0; i < E; ++i) {                                               \
+                const float t = at<T>(r_[c], i);                                                          \
+                v[c][i] = (expr_);                                                                        \
+            }                                                                                             \
+    }
+        RS_VEC(va, post_g);
+        RS_VEC(vb, post_b);
+        RS_VEC_GATE(vc);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = at<T>(w[c], i);
-        row_norm<G, MAXC>(v, p.post, p.post_eps, inv_d, nchunk, sub, s_red);
-#define RS_EACH(expr_)                                        \
-    _Pragma("unroll") for (int c = 0; c < MAXC; ++c)          \
-        _Pragma("unroll") for (int i = 0; i < 8; ++i) { const float t = at<T>(w[c], i); v[c][i] = (expr_); }
-        if (post_g) { vec(post_g); RS_EACH(v[c][i] * t) }
-        if (post_b) { vec(post_b); RS_EACH(v[c][i] + t) }
-        if (p.gate) { vec((const T*)p.gate + img * p.gate_stride); RS_EACH(v[c][i] * t) }
+        for (int c = 0; c < P; ++c)
 #pragma unroll
-        for (int c = 0; c < MAXC; ++c)
+            for (int i = 0; i < E; ++i) v[c][i] = at<T>(w[c], i);
+        row_norm<G, P, E>(v, p.post, p.post_eps, inv_d, n, sub, s_red);
+        RS_EACH(p.post_g, va, v[c][i] * t)
+        RS_EACH(p.post_b, vb, v[c][i] + t)
+        RS_EACH(p.gate, vc, v[c][i] * t)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = sub + c * G < nchunk ? fmaf(p.x_scale, at<T>(rx[c], i), p.f_scale * v[c][i]) : 0.f;
-        const bool on = row0 + my < p.rows;
-        const int64_t row = row0 + my;
-        if (p.y) {
+        for (int c = 0; c < P; ++c) {
 #pragma unroll
-            for (int c = 0; c < MAXC; ++c)
-                if (on && sub + c * G < nchunk) Elem<T>::store8((T*)p.y + row * D + (sub + c * G) * 8, v[c]);
+            for (int i = 0; i < E; ++i) v[c][i] = sub + c * G < n ? fmaf(p.x_scale, at<T>(rx[c], i), p.f_scale * v[c][i]) : 0.f;
+            if (p.y) store16_wt(rs_y, off[c], piece<T>(v[c]));
         }
         if (!p.u && !p.u_q) continue;
-        row_norm<G, MAXC>(v, p.pre, p.pre_eps, inv_d, nchunk, sub, s_red);
-        if (pre_g) { vec(pre_g); RS_EACH(v[c][i] * t) }
-        if (pre_b) { vec(pre_b); RS_EACH(v[c][i] + t) }
-        if (p.mod_scale) { vec((const T*)p.mod_scale + img * p.mod_stride); RS_EACH(fmaf(v[c][i], t, v[c][i])) }
-        if (p.mod_shift) { vec((const T*)p.mod_shift + img * p.mod_stride); RS_EACH(v[c][i] + t) }
+        RS_VEC(va, pre_g);
+        RS_VEC(vb, pre_b);
+        RS_VEC_MOD(vc, mod_scale);
+        RS_VEC_MOD(vd, mod_shift);
+        row_norm<G, P, E>(v, p.pre, p.pre_eps, inv_d, n, sub, s_red);
+        RS_EACH(p.pre_g, va, v[c][i] * t)
+        RS_EACH(p.pre_b, vb, v[c][i] + t)
+        RS_EACH(p.mod_scale, vc, fmaf(v[c][i], t, v[c][i]))
+        RS_EACH(p.mod_shift, vd, v[c][i] + t)
 #undef RS_EACH
+#undef RS_VEC
+#undef RS_VEC_GATE
+#undef RS_VEC_MOD
         if (p.u) {
 #pragma unroll
-            for (int c = 0; c < MAXC; ++c)
-                if (on && sub + c * G < nchunk) Elem<T>::store8((T*)p.u + row * D + (sub + c * G) * 8, v[c]);
+            for (int c = 0; c < P; ++c) store16_wt(rs_u, off[c], piece<T>(v[c]));
         }
         if (p.u_q) {
             float amax = 0.f;
 #pragma unroll
-            for (int c = 0; c < MAXC; ++c)
+            for (int c = 0; c < P; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[c][i] = sub + c * G < nchunk ? v[c][i] : 0.f;
+                for (int i = 0; i < E; ++i) {
+                    v[c][i] = sub + c * G < n ? v[c][i] : 0.f;
                     amax = amax_step(amax, v[c][i]);
                 }
             const QuantScale qs = quant_scale(row_reduce<G, true>(amax, s_red));
-            const int npad = (D + 15) / 16 * 2;  // zeros up to a multiple of 16
+            const int npad = (D + 15) / 16 * 16 / E;  // zeros up to a multiple of 16
 #pragma unroll
-            for (int c = 0; c < MAXC; ++c) {
-                const int ch = sub + c * G;
-                const uint2 b = make_uint2(quant8x4(v[c][0], v[c][1], v[c][2], v[c][3], qs), quant8x4(v[c][4], v[c][5], v[c][6], v[c][7], qs));
-                if (on && ch < npad) *reinterpret_cast<uint2*>(p.u_q + row * p.ldq + ch * 8) = b;
+            for (int c = 0; c < P; ++c) {
+                uint32_t b[E / 4];
+#pragma unroll
+                for (int h = 0; h < E / 4; ++h) b[h] = quant8x4(v[c][4 * h], v[c][4 * h + 1], v[c][4 * h + 2], v[c][4 * h + 3], qs);
+                if (on && sub + c * G < npad) {
+                    int8_t* q = p.u_q + row * p.ldq + (sub + c * G) * E;
+                    if constexpr (E == 8) *reinterpret_cast<uint2*>(q) = make_uint2(b[0], b[E / 4 - 1]);
+                    else *reinterpret_cast<uint32_t*>(q) = b[0];
+                }
             }
             if (on && sub == 0) p.u_scale[row] = qs.scale;
         }
     }
 }
 
-template <typename T, int G, int MAXC>
+template <typename T, int G, int P>
 static hipError_t go(const ResidualNormArgs& p, hipStream_t s) {
-    constexpr int RPB = G == 256 ? 1 : 256 / G;
+    constexpr int RPB = G > 64 ? 1 : 256 / G;
     const int64_t blocks = (p.rows + RPB - 1) / RPB;
-    hipLaunchKernelGGL((residual_norm_kernel<T, G, MAXC>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((residual_norm_kernel<T, G, P>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(G > 256 ? G : 256), 0, s, p);
     return hipGetLastError();
 }
 
-// The fewest lanes that hold a row in up to four chunks each: every lane busy at 192, 384 and 768 channels, where a wave per
-// row leaves a quarter to five eighths of its lanes without work.
+// The fewest lanes that hold a row in up to four pieces each: every lane busy at 192, 384 and 768 channels, where a wave per row
+// leaves a quarter to five eighths of its lanes without work.
 template <typename T>
 static hipError_t launch_rn(const ResidualNormArgs& p, hipStream_t s) {
-    const int D = p.D;
-    if (D <= 128) return go<T, 8, 2>(p, s);
-    if (D <= 192) return go<T, 8, 3>(p, s);
-    if (D <= 256) return go<T, 8, 4>(p, s);
-    if (D <= 384) return go<T, 16, 3>(p, s);
-    if (D <= 512) return go<T, 16, 4>(p, s);
-    if (D <= 768) return go<T, 32, 3>(p, s);
-    if (D <= 1024) return go<T, 32, 4>(p, s);
-    if (D <= 1536) return go<T, 64, 3>(p, s);
-    if (D <= 2048) return go<T, 64, 4>(p, s);
-    if (D <= 4096) return go<T, 256, 2>(p, s);
-    if (D <= 8192) return go<T, 256, 4>(p, s);
-    return go<T, 256, 8>(p, s);
+    const int n = p.D / kE<T>;
+    if (n <= 16) return go<T, 8, 2>(p, s);
+    if (n <= 24) return go<T, 8, 3>(p, s);
+    if (n <= 32) return go<T, 8, 4>(p, s);
+    if (n <= 48) return go<T, 16, 3>(p, s);
+    if (n <= 64) return go<T, 16, 4>(p, s);
+    if (n <= 96) return go<T, 32, 3>(p, s);
+    if (n <= 128) return go<T, 32, 4>(p, s);
+    if (n <= 192) return go<T, 64, 3>(p, s);
+    if (n <= 256) return go<T, 64, 4>(p, s);
+    if (n <= 512) return go<T, 256, 2>(p, s);
+    if (n <= 1024) return go<T, 256, 4>(p, s);
+    if constexpr (sizeof(T) == 4)  // D > 8192
+        if (n > 2048) return go<T, 1024, 4>(p, s);
+    return go<T, 512, 4>(p, s);
 }
 
 hipError_t launch_residual_norm(rs_dtype dt, const ResidualNormArgs& p, hipStream_t s) {

@@ -690,7 +690,8 @@ rs_status rs_residual_norm_fwd(const rs_residual_norm_cfg* cfg, const rs_residua
                "the eps of a norm must be positive");
     RS_REQUIRE(c.gate_stride >= 0 && c.mod_stride >= 0 && c.gate_stride % 8 == 0 && c.mod_stride % 8 == 0, RS_ERR_INVALID_ARG,
                "gate_stride and mod_stride must be multiples of 8 and not negative");
-    RS_REQUIRE(c.gate_stride <= kMaxPitch && c.mod_stride <= kMaxPitch, RS_ERR_UNSUPPORTED, "gate_stride or mod_stride > %lld", (long long)kMaxPitch);
+    RS_REQUIRE(c.gate_stride <= kResidualNormMaxStride && c.mod_stride <= kResidualNormMaxStride, RS_ERR_UNSUPPORTED,
+               "gate_stride or mod_stride > %d", kResidualNormMaxStride);
     RS_REQUIRE((c.post != RS_NORM_NONE || (!w->post_g && !w->post_b)) && (c.pre != RS_NORM_NONE || (!w->pre_g && !w->pre_b)),
                RS_ERR_INVALID_ARG, "the vectors of a norm that is not taken must be NULL");
     RS_REQUIRE(f || (c.post == RS_NORM_NONE && !w->gate), RS_ERR_INVALID_ARG, "post must be RS_NORM_NONE and gate NULL if f is NULL");
