@@ -168,7 +168,7 @@ def _stream(stream=None):
         if not torch.cuda.is_initialized():
             return None                  # nobody has chosen a stream yet: the default one
         # the handle alone: 0.3 us, through torch.cuda.current_stream() 3.4 of the 9.4 that a small call took
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -297,7 +297,7 @@ def rs_linear_fwd(a, w, bias, res, out, epi=RS_EPI_BIAS, stream=None) -> None:
 
 def _here(*tensors):
     """All on the current device, whose current stream the call goes to."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None   # None: nothing can be on a GPU yet
     for t in tensors:
         assert t is None or t.get_device() == dev, "every tensor must be on the current device"
 

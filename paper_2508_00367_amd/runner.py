@@ -1,4 +1,6 @@
-"""Launch sequence of a whole encoder stack: block after block through rs_block_fwd, ping-ponging two
+"""Launch sequences: a whole encoder stack (EncoderStack) and a block whose linear layers run in 8 bits (EncoderBlockI8).
+
+EncoderStack: block after block through rs_block_fwd, ping-ponging two
 activation buffers, optionally with the batch cut into parts that run on HIP streams of their own.
 
 Argument marshalling and buffer management only: every step of the computation runs inside the
@@ -112,3 +114,72 @@ class EncoderStack:
                 src[i] = dst
         K = self.P + self.sched[-1][1]
         return [s.view(-1)[:p["B"] * K * self.D].view(p["B"], K, self.D) for s, p in zip(src, self.parts)]
+
+
+class EncoderBlockI8:
+    """One encoder block whose four linear layers run in 8-bit integers, with token pruning behind it: the calls of the library in
+    their order, and the buffers between them.  Weights are quantized and packed once, here; activations on their way: the two norms
+    in front of the branches write 8-bit rows themselves, the attention's output and the hidden activations are quantized by a call.
+
+        x1   = x_scale x  + f_scale gate1 . Norm_post1(SA(Norm_1(x)))
+        xhat = x_scale x1 + f_scale gate2 . Norm_post2(MLP(Norm_2(x1)))
+        scores = D(MLP branch, x1);  y = the n_prefix first and the n_keep highest-scoring rows of xhat
+
+    `w`: name -> device tensor: the twelve tensors of rs_block_weights (biases, ln*_g and ln*_b may be missing) and, for encoders that
+    have them, post1_g, post1_b, gate1, post2_g, post2_b, gate2, all [D].  `norm`, `post`: RS_NORM_* in front of the
+    branches and behind them.  One object serves one stream at a time."""
+
+    def __init__(self, B: int, N: int, D: int, H: int, Dm: int, w: dict, n_prefix: int, n_keep: int, norm=rs.RS_NORM_LAYER,
+                 post=rs.RS_NORM_NONE, eps: float = 1e-6, x_scale: float = 1.0, f_scale: float = 1.0, dist=rs.RS_DIST_L2):
+        assert D == 64 * H, "heads are 64 wide"
+        self.B, self.N, self.D, self.H, self.Dm, self.P, self.n_keep, self.dist = B, N, D, H, Dm, n_prefix, n_keep, dist
+        dt, dev = w["w_qkv"].dtype, w["w_qkv"].device
+        self.layers = {k: self._pack(w["w_" + k], w.get("b_" + k)) for k in ("qkv", "proj", "fc1", "fc2")}
+        cfg = lambda post, pre: rs.make_residual_norm_cfg(B, N, D, dt, post, pre, eps, eps, x_scale, f_scale)  # noqa: E731
+        # in front of the attention: no branch yet, x as it is
+        self.first = (rs.make_residual_norm_cfg(B, N, D, dt, rs.RS_NORM_NONE, norm, eps, eps),
+                      rs.make_residual_norm_weights(dict(pre_g=w.get("ln1_g"), pre_b=w.get("ln1_b"))))
+        self.between = (cfg(post, norm), rs.make_residual_norm_weights(dict(
+            post_g=w.get("post1_g"), post_b=w.get("post1_b"), gate=w.get("gate1"), pre_g=w.get("ln2_g"), pre_b=w.get("ln2_b"))))
+        self.last = (cfg(post, rs.RS_NORM_NONE), rs.make_residual_norm_weights(dict(
+            post_g=w.get("post2_g"), post_b=w.get("post2_b"), gate=w.get("gate2"))))
+        M = B * N
+        new = lambda *s, dtype=dt: torch.empty(*s, dtype=dtype, device=dev)  # noqa: E731
+        self.q, self.q_scale = new(M, D, dtype=torch.int8), new(M, dtype=torch.float32)
+        self.hq, self.h_scale = new(M, (Dm + 15) // 16 * 16, dtype=torch.int8)[:, :Dm], new(M, dtype=torch.float32)
+        self.qkv, self.att, self.hid = new(B, N, 3, H, 64), new(B, N, H, 64), new(M, Dm)
+        self.branch, self.x1, self.xhat = new(M, D), new(B, N, D), new(B, N, D)
+        self.scores = new(B, N, dtype=torch.float32)
+        self.kept = new(B, n_prefix + n_keep, dtype=torch.int32)
+        self.y = new(B, n_prefix + n_keep, D)
+        self.ws = new(max(rs.rs_shift_topk_workspace_size(B, N, D, dt), 16), dtype=torch.uint8)
+
+    @staticmethod
+    def _pack(w: torch.Tensor, bias):
+        K, N = w.shape
+        q, scale = torch.empty_like(w, dtype=torch.int8), torch.empty(N, dtype=torch.float32, device=w.device)
+        rs.rs_quantize_columns(w, q, scale)
+        packed = torch.empty(rs.rs_packed_linear_i8_size(K, N), dtype=torch.uint8, device=w.device)
+        rs.rs_pack_linear_i8(q, packed)
+        return packed, scale, bias
+
+    def _linear(self, name: str, a, a_scale, out, epi=rs.RS_EPI_BIAS) -> None:
+        packed, scale, bias = self.layers[name]
+        rs.rs_linear_i8_fwd(a, a_scale, packed, scale, bias, None, out, epi)
+
+    def step(self, x: torch.Tensor):
+        """x [B, N, D] -> (y [B, n_prefix + n_keep, D], kept_idx, scores [B, N]): buffers of this object, valid until the next step."""
+        B, N, D, M = self.B, self.N, self.D, self.B * self.N
+        rs.rs_residual_norm_fwd(*self.first, x, None, None, None, self.q, self.q_scale)
+        self._linear("qkv", self.q, self.q_scale, self.qkv.view(M, 3 * D))
+        rs.rs_attention_fwd(self.qkv[:, :, 0], self.qkv[:, :, 1], self.qkv[:, :, 2], self.att, 0.125)
+        rs.rs_quantize_rows(self.att.view(M, D), self.q, self.q_scale)
+        self._linear("proj", self.q, self.q_scale, self.branch)
+        rs.rs_residual_norm_fwd(*self.between, x, self.branch, self.x1, None, self.q, self.q_scale)
+        self._linear("fc1", self.q, self.q_scale, self.hid, rs.RS_EPI_BIAS_GELU)
+        rs.rs_quantize_rows(self.hid, self.hq, self.h_scale)
+        self._linear("fc2", self.hq, self.h_scale, self.branch)
+        rs.rs_residual_norm_fwd(*self.last, self.x1, self.branch, self.xhat, None)
+        rs.rs_shift_topk(self.branch.view(B, N, D), self.x1, self.xhat, self.P, self.n_keep, self.scores, self.kept, self.y,
+                         self.dist, self.ws)
+        return self.y, self.kept, self.scores
