@@ -176,10 +176,16 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const Ep
 // ---------------------------------------------------------------------------
 // Direct kernel: workgroup tile 32 TM rows x 256 features, four waves of 32 TM x 64, two workgroups per CU.  Weights go from memory
 // straight into the registers of the one wave that needs them, the activations through a ring of four LDS stages of 128 k, copied
-// three slices ahead, as in gemm_bf16_direct_kernel, whose slices hold as many bytes.
+// three slices ahead, as in gemm_bf16_direct_kernel, whose slices hold as many bytes.  TM = 8, one workgroup per CU with 256
+// accumulator registers a lane: the weights of a slice serve twice the rows.
+// What bounds the large layers is the power the chip may draw: 32768 x 4096 -> 4096 runs at 1.6 GHz with the matrix cores busy 73 % of the
+// cycles, and a layer's time is the sum of what its products and its bytes cost (50432 x K -> 2304: 42 us + 0.088 us per k, 2.6 POPS; stores and
+// loads overlap in time but not in power; starting the second workgroup of a CU half a tile later changes nothing).  So the
+// kernel with the fewest bytes moved per product wins where it fills the chip.  (256 x 256 with waves of 128 x 128, half the LDS
+// reads but weights loaded by two waves each: 8192^3 423 -> 447 us.)
 // ---------------------------------------------------------------------------
 template <typename T, int EPI, bool RAGGED, int TM>
-__global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale,
+__global__ __launch_bounds__(256, TM == 8 ? 1 : 2) void gemm_i8_direct_kernel(const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale,
                                                                 const int8_t* __restrict__ w, const float* __restrict__ w_scale,
                                                                 const T* __restrict__ bias, const T* res, T* out, int64_t M, int N, int K,
                                                                 int tiles_m, int tiles_n, int gm) {
@@ -256,7 +262,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_direct_kernel(const int8_t* __
         _Pragma("unroll") for (int s_ = 0; s_ < TM; ++s_) {                                               \
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                            \
             __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);                                           \
-            __builtin_amdgcn_sched_group_barrier(0x020, 4 / TM, 0);                                       \
+            __builtin_amdgcn_sched_group_barrier(0x020, TM == 2 ? 2 : 1, 0);                              \
         }                                                                                                 \
         __builtin_amdgcn_sched_barrier(0);                                                                \
     }
@@ -647,7 +653,7 @@ template <typename T, int EPI, bool RAGGED, int TM>
 static void launch_i8_direct(const GemmI8Args& g, hipStream_t s) {
     const int tiles_m = (int)((g.M + 32 * TM - 1) / (32 * TM)), tiles_n = (g.N + 255) / 256, nblk = tiles_m * tiles_n;
     hipLaunchKernelGGL((gemm_i8_direct_kernel<T, EPI, RAGGED, TM>), dim3(8 * ((nblk + 7) / 8)), dim3(256), 0, s, g.a, (int)g.lda, g.a_scale,
-                       (const int8_t*)g.w, g.w_scale, (const T*)g.bias, (const T*)g.res, (T*)g.out, g.M, g.N, g.K, tiles_m, tiles_n, 16);
+                       (const int8_t*)g.w, g.w_scale, (const T*)g.bias, (const T*)g.res, (T*)g.out, g.M, g.N, g.K, tiles_m, tiles_n, TM == 8 ? 8 : 16);  // row panels that pass together
 }
 
 template <typename T, int EPI, bool RAGGED>
@@ -672,6 +678,7 @@ static void launch_i8_part(const GemmI8Args& g, hipStream_t s) {
         case GemmI8Tile::Private64x64: launch_i8_private<T, EPI, RAGGED>(g, s); break;
         case GemmI8Tile::Direct64x256: launch_i8_direct<T, EPI, RAGGED, 2>(g, s); break;
         case GemmI8Tile::Direct128x256: launch_i8_direct<T, EPI, RAGGED, 4>(g, s); break;
+        case GemmI8Tile::Direct256x256: launch_i8_direct<T, EPI, RAGGED, 8>(g, s); break;
     }
 }
 

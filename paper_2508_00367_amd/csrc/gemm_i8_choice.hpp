@@ -5,7 +5,7 @@
 
 namespace rs {
 
-enum class GemmI8Tile { Split32x32, Split32x64, Private64x64, Direct64x256, Direct128x256 };
+enum class GemmI8Tile { Split32x32, Split32x64, Private64x64, Direct64x256, Direct128x256, Direct256x256 };
 
 // By the number of tiles and the length of K.  us per launch, bf16 output with bias, operands out of the caches in turn:
 //  - Up to one 32 x 32 tile per CU: the split kernel, which has the shortest way through (32 x 32 / 32 x 64 / private / direct 128 x 256: 768 -> 2304 at one row
@@ -21,12 +21,17 @@ enum class GemmI8Tile { Split32x32, Split32x64, Private64x64, Direct64x256, Dire
 //       round (4400 x 1024 -> 4096 25.9 / 28.0, 16388 x 1024 -> 1024 25.7 / 26.9; at 1.1 of K = 2048 a tie);
 //     . up to two rounds at K <= 768, where a tile is mostly its ends (9000 x 768 -> 2304 22.8 / 24.9, 12608 x 384 -> 1536 15.3 / 18.5, 25216 x 768 -> 768 22.6 / 24.1), but
 //       for one round nearly full (9000 x 384 -> 1536 13.6 / 11.3).
+//     . 256 rows a tile, one per CU, at K >= 2048 where the last round of them is full or at least 0.7 so (128 / 256 rows a tile: 16384 x 2048 -> 2048 69.8 / 67.7,
+//       16384 x 8192 -> 2048 232 / 216, 14000 x 4096 -> 1024 (0.86) 61 / 57, 12000 x 8192 -> 1024 (0.73) 98 / 93, 32768 x 4096 -> 4096 465 / 449; 1.5 rounds: 6000 x
+//       4096 -> 4096 88 / 101; 16388 x 1024 -> 4096 80 / 97: a shorter K leaves the tile's ends uncovered).
 inline GemmI8Tile gemm_i8_choose(int64_t M, int64_t N, int K, int64_t cus) {
     auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     if (tiles(32, 32) <= cus) return GemmI8Tile::Split32x32;
     if (K <= 1024 && tiles(32, 64) <= cus) return GemmI8Tile::Split32x64;
     const int64_t t64 = tiles(64, 64);
     if (t64 <= cus || (K >= 1024 && t64 <= 2 * cus)) return GemmI8Tile::Private64x64;
+    const int64_t last = tiles(256, 256) % cus;
+    if (K >= 2048 && (last == 0 || 10 * last >= 7 * cus)) return GemmI8Tile::Direct256x256;
     const int64_t t = tiles(128, 256);
     if (tiles(64, 256) <= cus || (t > cus && 4 * t <= 5 * cus) || (t > 2 * cus && 10 * t <= 23 * cus)) return GemmI8Tile::Direct64x256;
     if (K <= 768 && t <= 4 * cus && !(2 * t > 3 * cus && t <= 2 * cus)) return GemmI8Tile::Direct64x256;

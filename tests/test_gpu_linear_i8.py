@@ -80,7 +80,7 @@ def test_linear_i8(M, K, N, epi, dtype):
 
 # One size for each kernel, rows of whole 16-byte pieces and others: tests/test_i8_choice_cpu.py has which is which.
 EVERY_KERNEL = [(40, 300, 200), (197, 768, 2304), (197, 770, 1155), (788, 768, 768), (900, 200, 1001), (788, 4096, 1024), (1576, 768, 2304),
-                (1700, 1300, 2051), (1576, 1024, 4096), (2500, 1100, 3001)]
+                (1700, 1300, 2051), (1576, 1024, 4096), (2500, 1100, 3001), (3000, 2048, 4096), (3000, 2100, 4001)]
 
 
 @pytest.mark.parametrize("epi,dtype", [("bias", "bf16"), ("gelu", "bf16"), ("res", "bf16"), ("res", "f32"), ("gelu", "f32")])
@@ -97,7 +97,7 @@ def test_every_kernel(M, K, N, epi, dtype):
 
 
 @pytest.mark.parametrize("K", [1, 127, 128, 129, 640, 1024, 1025, 2048, 3200, 5000, 9000])
-@pytest.mark.parametrize("M,N", [(33, 70), (300, 1100), (1100, 3000)])
+@pytest.mark.parametrize("M,N", [(33, 70), (300, 1100), (1100, 3000), (2900, 4000)])
 def test_every_length_of_the_inner_axis(M, N, K):
     """Rings and peeled tails of every kernel, from one slice to many; exact sums, so every row is the same where the rows are."""
     _say("inner axis", M, K, N)
