@@ -24,8 +24,8 @@ __device__ __forceinline__ float gelu_of(float x, const bf16raw*) { return gelu_
 // 32 i + 8 q + 4 g + e in register 4 q + e of acc[i][j].  Only the traffic with memory goes through LDS, one 4 KB region (32 rows of
 // 128 bytes) per 32-row group: residual rows arrive there by direct copies, a lane picks up its 4 features and puts the result
 // back in place, the group leaves as 16 bytes per lane in whole row segments.  In bf16 a region holds the wave's 64 features, in
-// fp32 32 of them, and the features go in two passes.  Rows of `out` that are not whole 16-byte pieces (RAGGED) are
-// read and written an element per lane.
+// fp32 32 of them, and the features go in two passes.  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
+// anywhere (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 7).
 // ---------------------------------------------------------------------------
 template <typename T> struct EpiI8 {
     static constexpr int PASSES = sizeof(T) / 2;        // over the wave's 64 features
@@ -57,6 +57,32 @@ __device__ __forceinline__ int region_at(int r, int f) {  // byte of feature f (
     return r * 128 + (((b >> 4) ^ epi_swz(r)) << 4) + (b & 15);
 }
 
+// Piece c of a row that starts anywhere, of which `n` elements are inside: 16 bytes at an address aligned to the element only (which
+// the hardware takes), the last elements one by one.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Piece16 { u32x4 v; };
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* row, int c, int n) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if ((c + 1) * E <= n) return reinterpret_cast<const Piece16<T>*>(row + c * E)->v;
+    struct { T e[E]; } w;
+#pragma unroll
+    for (int i = 0; i < E; ++i) w.e[i] = c * E + i < n ? row[c * E + i] : T{};
+    return __builtin_bit_cast(u32x4, w);
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, int c, int n, u32x4 v) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if ((c + 1) * E <= n) {
+        reinterpret_cast<Piece16<T>*>(row + c * E)->v = v;
+        return;
+    }
+    struct W { T e[E]; };
+    const W w = __builtin_bit_cast(W, v);
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (c * E + i < n) row[c * E + i] = w.e[i];
+}
+
 // Residual rows of one pass into the regions; rows past M read as zeros, pieces past N are of the next row and not used.
 template <typename T, int TM, bool RAGGED>
 __device__ __forceinline__ void i8_request_res(const EpiRegions<TM>& reg, const T* res, int64_t M, int N, int64_t m_base, int n,
@@ -66,10 +92,11 @@ __device__ __forceinline__ void i8_request_res(const EpiRegions<TM>& reg, const 
     const int rows = (int)(left < 32 * TM ? left : 32 * TM);
     const T* base = res + m_base * N + n;
     if constexpr (RAGGED) {
-        constexpr int F = EpiI8<T>::F, RPI = 64 / F;
-        const int f = lane % F;
-        for (int r = lane / F; r < rows; r += RPI)
-            if (n + f < N) *reinterpret_cast<T*>(reg.r[0] + (r >> 5) * 4096 + region_at<T>(r & 31, f)) = base[(int64_t)r * N + f];
+#pragma unroll
+        for (int p = 0; p < 4 * TM; ++p) {
+            const int r = p * 8 + (lane >> 3), c = lane & 7;
+            if (r < rows) *reinterpret_cast<u32x4*>(reg.r[p >> 2] + (r & 31) * 128 + ((c ^ epi_swz(r & 31)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
+        }
     } else {
         const int64_t bytes = ((int64_t)(rows - 1) * N + min(N - n, EpiI8<T>::F)) * (int)sizeof(T);
         const __amdgpu_buffer_rsrc_t rs_res = make_rsrc(base, bytes);
@@ -154,11 +181,11 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const Ep
                 }
             // the group leaves (LDS accesses of one wave are served in order)
             if constexpr (RAGGED) {
-                constexpr int RPI = 64 / F;
-                const int f = lane % F;
-                for (int r = lane / F; r < 32 && j * 32 + r < rows; r += RPI) {
-                    const T v = *reinterpret_cast<const T*>(buf + region_at<T>(r, f));
-                    if (n + f < N) out[(m_base + j * 32 + r) * N + n + f] = v;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int r = s * 8 + (lane >> 3), c = lane & 7;
+                    if (j * 32 + r < rows)
+                        store_piece(out + (m_base + j * 32 + r) * N + n, c, N - n, *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4)));
                 }
             } else {
 #pragma unroll

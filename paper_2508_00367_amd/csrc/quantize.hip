@@ -128,7 +128,7 @@ static void by_width(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* 
         if (K <= 256) RS_Q(16, 1, true, false);
         else if (K <= 512) RS_Q(32, 1, true, false);
         else if (K <= 1024) RS_Q(64, 1, true, false);
-        else if (K <= 2048 && sizeof(T) == 2) RS_Q(64, 2, true, false);
+        else if (K <= 2048 && sizeof(T) == 2 && M >= 4096) RS_Q(64, 2, true, false);
         else if (K <= 4096) RS_Q(256, 1, true, false);
         else if (K <= 16384) RS_Q(256, 4, true, false);
         else RS_Q(256, 1, true, true);

@@ -198,6 +198,10 @@ static hipError_t go(const ResidualNormArgs& p, hipStream_t s) {
 template <typename T>
 static hipError_t launch_rn(const ResidualNormArgs& p, hipStream_t s) {
     const int n = p.D / kE<T>;
+    const int64_t cus = device_cus();
+    if (n <= 32 && p.rows <= 16 * cus) return go<T, 32, 1>(p, s);
+    if (n > 32 && n <= 64 && p.rows <= 8 * cus) return go<T, 64, 1>(p, s);
+    if (n > 64 && n <= 256 && p.rows <= 4 * cus) return go<T, 256, 1>(p, s);
     if (n <= 16) return go<T, 8, 2>(p, s);
     if (n <= 24) return go<T, 8, 3>(p, s);
     if (n <= 32) return go<T, 8, 4>(p, s);
