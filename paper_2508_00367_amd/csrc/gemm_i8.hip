@@ -657,7 +657,9 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_private_kernel(
     if (wave >= TM) return;
     i32x16 sum[TN][1];
 #pragma unroll
-    for (int i = 0; i < TN; ++i) sum[i][0] = wave == 0 ? acc[i][0] : acc[i][1];
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[i][0][r] = wave == 0 ? acc[i][0][r] : acc[i][1][r];  // (a choice of whole vectors goes through scratch memory)
 #pragma unroll
     for (int o = 0; o < W - 1; ++o) {
         const unsigned char* s = slot(wave, o);
