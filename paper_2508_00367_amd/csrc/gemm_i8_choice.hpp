@@ -14,6 +14,9 @@ enum class GemmI8Tile { Split32x32, Split32x64, Private64x64, Direct64x256, Dire
 //    8.2); at K = 4096 its operands, which come in pieces of lines, cost more than that (394 x 4096 -> 1024 13.0 / 10.4 / 9.7 / 21.9).
 //  - Up to one 64 x 64 tile per CU, two where K >= 1024: the private kernel (private / direct 64 x 256 / direct 128 x 256: 768 x 768 at 788 rows 5.0 / 6.1 / 8.4, at
 //    2200 (420 tiles) 7.0 / 6.2 / 8.4; 4096 -> 1024 at 1576 (400) 15.0 / 18.2 / 22.4, at 2200 (560) 20.9 / 18.6 / 22.6; 1024 -> 4096 at 394 (448) 6.7 / 6.8 / 9.3).
+//  - At most 64 features and K >= 512, or 128 and K >= 2048: the private kernel for any number of rows, the direct one's tiles being mostly empty (private / direct
+//    64 x 256 / direct 128 x 256: 768 -> 64 at 50432 rows 13.7 / 16.4 / 15.2, 4096 -> 64 at 25000 26 / 34 / 34, 2048 -> 128 at 34508 22.0 / 24.1 / 25.7; but 192 -> 64 at
+//    50432 8.1 / 8.3 / 7.6, 768 -> 128 there 19.3 / 17.4 / 15.7).
 //  - Beyond: the direct kernel.  Two of its 128 x 256 tiles run on a CU at a time and feed the matrix cores best (50432 x 768 -> 768, 64 / 128 rows a tile, 48 / 41; 12552 x
 //    4096 -> 1024 64 / 52; 32768 x 4096 -> 4096 580 / 462), but a grid that is not many rounds of them leaves CUs idle at its end.  64 rows a tile:
 //     . up to one such tile per CU (1576 x 768 -> 2304 7.6 / 9.8, 3152 x 4096 -> 1024 19.4 / 22.8);
@@ -30,6 +33,7 @@ inline GemmI8Tile gemm_i8_choose(int64_t M, int64_t N, int K, int64_t cus) {
     if (K <= 1024 && tiles(32, 64) <= cus) return GemmI8Tile::Split32x64;
     const int64_t t64 = tiles(64, 64);
     if (t64 <= cus || (K >= 1024 && t64 <= 2 * cus)) return GemmI8Tile::Private64x64;
+    if ((N <= 64 && K >= 512) || (N <= 128 && K >= 2048)) return GemmI8Tile::Private64x64;
     const int64_t last = tiles(256, 256) % cus;
     if (K >= 2048 && (last == 0 || 10 * last >= 7 * cus)) return GemmI8Tile::Direct256x256;
     const int64_t t = tiles(128, 256);

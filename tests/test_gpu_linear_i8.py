@@ -268,3 +268,45 @@ def test_captured_and_replayed():
         call(eager)
         torch.cuda.synchronize()
         assert torch.equal(got, eager), i
+
+
+def test_offsets_past_32_bits():
+    """Outputs of 2.4e9 elements; activations whose rows lie 2 MiB apart over 2.3 GB; the last rows and columns against 64 bits."""
+    M, K, N = 60000, 16, 40000
+    a, a_s, w, w_s, bias, _ = make(M, K, N, "bf16", "bias", 31)
+    out = torch.full((M, N), -777.0, dtype=torch.bfloat16, device="cuda")
+    rs.rs_linear_i8_fwd(a, a_s, packed(w), w_s, bias, None, out)
+    for rows in (slice(0, 3), slice(53686, 53690), slice(M - 3, M)):   # element 2^31 lies in row 53687
+        check(out[rows], a[rows], a_s[rows], w, w_s, bias, None, "bf16", "bias")
+    del out
+    far = torch.full((1100, 1 << 21), 55, dtype=torch.int8, device="cuda")
+    a2, a2_s, w2, w2_s, b2, _ = make(1100, 64, 96, "f32", "bias", 32)
+    far[:, :64] = a2
+    check(run_linear(far[:, :64], a2_s, w2, w2_s, b2, None, "f32", "bias"), a2, a2_s, w2, w2_s, b2, None, "f32", "bias")
+
+
+def test_quantize_rows_past_32_bits():
+    M, K = 1100000, 2048
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    x.normal_()
+    q, scale = torch.full((M + 1, K), 55, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    rs.rs_quantize_rows(x, q[:M], scale)
+    for rows in (slice(0, 4), slice(1048574, 1048580), slice(M - 4, M)):
+        rq, rscale = quantize(x[rows].float().cpu().numpy(), 1)
+        assert np.array_equal(q[rows].cpu().numpy(), rq) and np.array_equal(scale[rows].cpu().numpy(), rscale)
+    assert bool((q[M] == 55).all())
+
+
+def test_two_streams_at_once():
+    """No workspace, nothing shared: two calls that overlap in time give what each gives alone."""
+    t = [make(900, 1024, 1000, "bf16", "gelu", s) for s in (41, 42)]
+    alone = [run_linear(*x, "bf16", "gelu") for x in t]
+    pws = [packed(x[2]) for x in t]
+    outs = [torch.empty_like(o) for o in alone]
+    streams = [torch.cuda.Stream() for _ in t]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, pw, o, s in zip(t, pws, outs, streams):
+            rs.rs_linear_i8_fwd(x[0], x[1], pw, x[3], x[4], None, o, rs.RS_EPI_BIAS_GELU, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))

@@ -187,3 +187,33 @@ def test_captured_and_replayed():
         rs.rs_residual_norm_fwd(cfg, w, x, f, ey, eu)
         torch.cuda.synchronize()
         assert torch.equal(gy, ey) and torch.equal(gu, eu), i
+
+
+def test_offsets_past_32_bits():
+    """2.25e9 elements a tensor, 8-bit rows far apart; the rows on both sides of element 2^31 and the last ones."""
+    N, D = 1100000, 2048
+    x = torch.empty(1, N, D, dtype=torch.bfloat16, device="cuda").normal_()
+    f = torch.empty_like(x).normal_()
+    v = {n: t for n, t in make(1, 1, D, "bf16", False, 5)[2].items()}
+    cfg = rs.make_residual_norm_cfg(1, N, D, torch.bfloat16, rs.RS_NORM_LAYER, rs.RS_NORM_RMS, 1e-6, 1e-5, 1.0, 1.0)
+    y, u_q, u_s = torch.empty_like(x), torch.empty(N, D + 16, dtype=torch.int8, device="cuda"), torch.empty(N, device="cuda")
+    rs.rs_residual_norm_fwd(cfg, rs.make_residual_norm_weights(v), x, f, y, None, u_q[:, :D], u_s)
+    for rows in (slice(0, 4), slice(1048574, 1048580), slice(N - 4, N)):
+        ry, ru, ey, eu = reference(x[:, rows], f[:, rows], v, "layer", "rms", False, 1.0, 1.0)
+        within(y[:, rows], ry, ey, "bf16")
+        check8(u_q[rows], u_s[rows], ru, eu, D)
+
+
+@pytest.mark.parametrize("D", [64, 256, 264, 512, 520, 1024, 2048, 2056])
+@pytest.mark.parametrize("rows", [1, 3, 1023, 1025, 2047, 2050, 4095, 4099])
+def test_every_number_of_lanes(rows, D):
+    """Rows on more lanes where there are few of them: the sizes on both sides of each step, every image its own vectors, one row each."""
+    x, f, v, stride = make(rows, 1, D, "bf16", True, seed=rows + D)
+    cfg = rs.make_residual_norm_cfg(rows, 1, D, torch.bfloat16, rs.RS_NORM_LAYER, rs.RS_NORM_LAYER, 1e-6, 1e-5, 0.5, 2.0, stride, stride)
+    y, u = torch.empty_like(x), torch.empty_like(x)
+    u_q, u_s = torch.empty(rows, (D + 15) // 16 * 16, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    rs.rs_residual_norm_fwd(cfg, rs.make_residual_norm_weights(v), x, f, y, u, u_q[:, :D], u_s)
+    ry, ru, ey, eu = reference(x, f, v, "layer", "layer", True, 0.5, 2.0)
+    within(y, ry, ey, "bf16")
+    within(u, ru, eu, "bf16")
+    check8(u_q, u_s, ru, eu, D)

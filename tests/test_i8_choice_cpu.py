@@ -45,6 +45,7 @@ MEASURED = [((1, 768, 2304), "split32x32"), ((64, 768, 2304), "split32x32"), ((1
             ((9000, 768, 2304), "direct64"), ((12608, 384, 1536), "direct64"), ((25216, 768, 768), "direct64"), ((9000, 384, 1536), "direct128"),
             ((1576, 1024, 4096), "direct128"), ((3152, 2048, 2048), "direct128"), ((50432, 768, 768), "direct128"), ((50432, 768, 2304), "direct128"),
             ((16388, 1024, 4096), "direct128"), ((12552, 4096, 1024), "direct256"), ((32768, 4096, 4096), "direct256"),
+            ((50432, 768, 64), "private"), ((34508, 2048, 128), "private"), ((50432, 192, 64), "direct128"), ((50432, 768, 128), "direct128"),
             ((6000, 4096, 4096), "direct128"), ((16384, 2048, 2048), "direct256"), ((20000, 4096, 1024), "direct128"), ((14000, 4096, 1024), "direct256")]
 
 

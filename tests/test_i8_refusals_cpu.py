@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2508_00367_amd as rs
 from paper_2508_00367_amd import binding
@@ -108,3 +109,15 @@ def test_null_structs_and_empty_calls():
         assert L.rs_residual_norm_fwd(ctypes.byref(cfg), ctypes.byref(w), None, P[1], P[2], P[3], None, 0, None, None) == rs.RS_OK
     assert L.rs_quantize_rows(None, 0, 96, 96, rs.RS_BF16, None, 96, None, None) == rs.RS_OK
     assert L.rs_linear_i8_fwd(None, 96, None, None, None, None, None, None, 0, 64, 96, rs.RS_EPI_BIAS, rs.RS_BF16, None) == rs.RS_OK
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
+    f, q, s = torch.zeros(4, 16), torch.zeros(4, 16, dtype=torch.int8), torch.zeros(4)
+    cfg = rs.make_residual_norm_cfg(1, 4, 16, rs.RS_F32)
+    for call in (lambda: rs.rs_quantize_rows(f, q, s), lambda: rs.rs_quantize_columns(f, q, torch.zeros(16)),
+                 lambda: rs.rs_pack_linear_i8(q, torch.zeros(1 << 14, dtype=torch.uint8)),
+                 lambda: rs.rs_linear_i8_fwd(q, s, torch.zeros(1 << 14, dtype=torch.uint8), s, None, None, torch.zeros(4, 4)),
+                 lambda: rs.rs_residual_norm_fwd(cfg, rs.make_residual_norm_weights({}), f, None, None, f.clone()),
+                 lambda: rs.make_residual_norm_weights(dict(pre_g=torch.ones(16)))):
+        with pytest.raises(AssertionError, match="device"):
+            call()
