@@ -27,9 +27,10 @@ __device__ __forceinline__ float gelu_of(float x, const bf16raw*) { return gelu_
 // fp32 32 of them, and the features go in two passes.  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
 // anywhere (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 7).
 // ---------------------------------------------------------------------------
-template <typename T> struct EpiI8 {
-    static constexpr int PASSES = sizeof(T) / 2;        // over the wave's 64 features
-    static constexpr int F = 64 / PASSES;               // features of a region
+template <typename T, int TN> struct EpiI8 {              // a wave of 32 TN features
+    static constexpr int F = sizeof(T) == 4 ? 32 : 32 * TN;  // features of a region
+    static constexpr int PASSES = 32 * TN / F;
+    static constexpr int PIECES = F * (int)sizeof(T) / 16;   // of a row: 8, or 4 in half-filled regions (bf16, TN = 1)
 };
 
 // w_scale, bias and a_scale of a tile in LDS: 256 features in fp32, 256 of T, 256 rows.
@@ -84,7 +85,7 @@ __device__ __forceinline__ void store_piece(T* row, int c, int n, u32x4 v) {
 }
 
 // Residual rows of one pass into the regions; rows past M read as zeros, pieces past N are of the next row and not used.
-template <typename T, int TM, bool RAGGED>
+template <typename T, int TM, bool RAGGED, int F>
 __device__ __forceinline__ void i8_request_res(const EpiRegions<TM>& reg, const T* res, int64_t M, int N, int64_t m_base, int n,
                                                int lane) {
     const int64_t left = M - m_base;
@@ -98,7 +99,7 @@ __device__ __forceinline__ void i8_request_res(const EpiRegions<TM>& reg, const 
             if (r < rows) *reinterpret_cast<u32x4*>(reg.r[p >> 2] + (r & 31) * 128 + ((c ^ epi_swz(r & 31)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
         }
     } else {
-        const int64_t bytes = ((int64_t)(rows - 1) * N + min(N - n, EpiI8<T>::F)) * (int)sizeof(T);
+        const int64_t bytes = ((int64_t)(rows - 1) * N + min(N - n, F)) * (int)sizeof(T);
         const __amdgpu_buffer_rsrc_t rs_res = make_rsrc(base, bytes);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -134,9 +135,9 @@ __device__ __forceinline__ f32x4 bias4(const unsigned char* at, const float*) { 
 
 // `vec`: the tile's vectors (landed); row0 and f0: the wave's first row and feature inside the tile.  The regions are this wave's
 // own and consecutive 4 KB apart (one array per wave).
-template <typename T, int EPI, int TM, bool RAGGED>
-__device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const EpiRegions<TM>& reg, const unsigned char* vec, const T* res, T* out, int64_t M, int N, int64_t m_base, int n_base, int row0, int f0, int lane) {
-    constexpr int P = EpiI8<T>::PASSES, F = EpiI8<T>::F;
+template <typename T, int EPI, int TM, bool RAGGED, int TN>
+__device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const EpiRegions<TM>& reg, const unsigned char* vec, const T* res, T* out, int64_t M, int N, int64_t m_base, int n_base, int row0, int f0, int lane) {
+    constexpr int P = EpiI8<T, TN>::PASSES, F = EpiI8<T, TN>::F, NI = TN / P, PIECES = EpiI8<T, TN>::PIECES;
     const int l32 = lane & 31, g = lane >> 5;
     if (n_base >= N || m_base >= M) return;
     float as[TM];
@@ -149,12 +150,12 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const Ep
         if (n >= N) break;
         if (EPI == EPI_BIAS_RES) {
             if (p > 0) __builtin_amdgcn_s_waitcnt(0xC07F);  // what the last pass reads from the regions has been read
-            i8_request_res<T, TM, RAGGED>(reg, res, M, N, m_base, n, lane);
+            i8_request_res<T, TM, RAGGED, F>(reg, res, M, N, m_base, n, lane);
             __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & 0xC07F);  // every residual row of the pass has landed
         }
-        f32x4 ws[2 / P][4], bv[2 / P][4];
+        f32x4 ws[NI][4], bv[NI][4];
 #pragma unroll
-        for (int i = 0; i < 2 / P; ++i)
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int f = f0 + p * F + i * 32 + q * 8 + g * 4;
@@ -166,32 +167,27 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[2][TM], const Ep
         for (int j = 0; j < TM; ++j) {
             unsigned char* buf = reg.r[j];
 #pragma unroll
-            for (int i = 0; i < 2 / P; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     unsigned char* at = buf + region_at<T>(l32, i * 32 + q * 8 + g * 4);
                     float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[e] = fmaf((float)acc[P == 2 ? p : i][j][4 * q + e], as[j] * ws[i][q][e], bv[i][q][e]);
+                        v[e] = fmaf((float)acc[P > 1 ? p : i][j][4 * q + e], as[j] * ws[i][q][e], bv[i][q][e]);
                         if (EPI == EPI_BIAS_GELU) v[e] = gelu_of(v[e], (const T*)nullptr);
                     }
                     if (EPI == EPI_BIAS_RES) res_add(v, at, (const T*)nullptr);
                     put4(at, v, (T*)nullptr);  // in place: this lane alone reads and writes these bytes
                 }
             // the group leaves (LDS accesses of one wave are served in order)
-            if constexpr (RAGGED) {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int r = s * 8 + (lane >> 3), c = lane & 7;
-                    if (j * 32 + r < rows)
-                        store_piece(out + (m_base + j * 32 + r) * N + n, c, N - n, *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4)));
-                }
-            } else {
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int r = s * 8 + (lane >> 3), c = lane & 7;
-                    const u32x4 o4 = *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4));
+            for (int s = 0; s < PIECES / 2; ++s) {
+                const int r = s * (64 / PIECES) + lane / PIECES, c = lane % PIECES;
+                const u32x4 o4 = *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4));
+                if constexpr (RAGGED) {
+                    if (j * 32 + r < rows) store_piece(out + (m_base + j * 32 + r) * N + n, c, N - n, o4);
+                } else {
                     const bool in = j * 32 + r < rows && n + c * (16 / (int)sizeof(T)) < N;
                     store16_wt(rs_out, in ? ((j * 32 + r) * N) * (int)sizeof(T) + c * 16 : kPastEnd, o4);
                 }
@@ -369,7 +365,7 @@ __global__ __launch_bounds__(256, TM == 8 ? 1 : 2) void gemm_i8_direct_kernel(co
     unsigned char* const base = wave == 0 ? st0 : wave == 1 ? st1 : wave == 2 ? st2 : st3;
 #pragma unroll
     for (int j = 0; j < TM; ++j) reg.r[j] = base + j * 4096;
-    i8_epilogue<T, EPI, TM, RAGGED>(acc, reg, s_vec, res, out, M, N, m0, n_base, 0, wave * 64, lane);
+    i8_epilogue<T, EPI, TM, RAGGED, TN>(acc, reg, s_vec, res, out, M, N, m0, n_base, 0, wave * 64, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -499,7 +495,8 @@ __global__ __launch_bounds__(512, TN > 1 ? 2 : 4) void gemm_i8_split_kernel(
 // ---------------------------------------------------------------------------
 // Private kernel, for grids in between: 64 rows x 64 features, the slices of K dealt out to four waves, each with two stages of
 // its own for the rows (whole lines by direct copies) and its weights in registers: no barrier before the sums meet.  They
-// do so in LDS, where the first two waves collect the 32-row group that they then write.  Two workgroups per CU.
+// do so in LDS, where each wave collects the 32 x 32 block that it then writes (two waves, 32 rows each: 1003 x 588 -> 1000 fp32 with
+// GELU 8.8 us, so 7.1).  Two workgroups per CU.
 // (128 rows, one workgroup per CU: 512 x 4096 -> 4096 15.2 -> 13.9 us, where every CU has one such tile, elsewhere slower: 788 x 768 -> 2304
 // 6.4 -> 6.8, 1576 x 4096 -> 1024 the same.)
 // ---------------------------------------------------------------------------
@@ -634,48 +631,45 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_private_kernel(
 #undef RS_I8_MFMA
 #undef RS_I8_COMPUTE
 #undef RS_I8_WAIT
-    // Group j of the tile goes to wave j: the others leave theirs in slots of 8 KB, [group][other wave], 16 bytes per lane.
+    // Wave f collects 32 x 32 block f, features 32 (f / 2) .. of rows 32 (f % 2) ..: the others leave theirs in slots of
+    // 4 KB, [block][other wave], 16 bytes per lane.
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & 0xC07F);  // the vectors have landed
     __syncthreads();  // every wave has read its stages
-    constexpr int PER = W * STAGE / 8192;  // slots of a stage array
-    static_assert(TM * (W - 1) <= 2 * PER, "slots");
-    auto slot = [&](int j, int from) {
-        const int at = j * (W - 1) + from;
-        return (at < PER ? st0 + at * 8192 : st1 + (at - PER) * 8192) + lane * 16;
+    static_assert(TM * TN == W && W * (W - 1) * 4096 <= 2 * W * STAGE, "a block for each wave, slots in the stages");
+    constexpr int PER = W * STAGE / 4096;  // slots of a stage array
+    auto slot = [&](int f, int from) {
+        const int at = f * (W - 1) + from;
+        return (at < PER ? st0 + at * 4096 : st1 + (at - PER) * 4096) + lane * 16;
     };
+    i32x16 sum[1][1];
 #pragma unroll
-    for (int j = 0; j < TM; ++j)
-        if (j != wave) {
-            unsigned char* s = slot(j, wave - (wave > j ? 1 : 0));
+    for (int f = 0; f < W; ++f) {
+        const i32x16& own = acc[f >> 1][f & 1];
+        if (f == wave) {
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
+            for (int r = 0; r < 16; ++r) sum[0][0][r] = own[r];
+        } else {
+            unsigned char* s = slot(f, wave - (wave > f ? 1 : 0));
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<i32x4*>(s + (i * 4 + q) * 1024) = i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<i32x4*>(s + q * 1024) = i32x4{own[4 * q], own[4 * q + 1], own[4 * q + 2], own[4 * q + 3]};
         }
+    }
     __syncthreads();
-    if (wave >= TM) return;
-    i32x16 sum[TN][1];
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[i][0][r] = wave == 0 ? acc[i][0][r] : acc[i][1][r];  // (a choice of whole vectors goes through scratch memory)
 #pragma unroll
     for (int o = 0; o < W - 1; ++o) {
         const unsigned char* s = slot(wave, o);
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
+        for (int q = 0; q < 4; ++q) {
+            const i32x4 v = *reinterpret_cast<const i32x4*>(s + q * 1024);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const i32x4 v = *reinterpret_cast<const i32x4*>(s + (i * 4 + q) * 1024);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum[i][0][4 * q + e] += v[e];
-            }
+            for (int e = 0; e < 4; ++e) sum[0][0][4 * q + e] += v[e];
+        }
     }
     EpiRegions<1> reg;
     reg.r[0] = slot(wave, 0) - lane * 16;  // read by this wave alone, and it has been read
     __builtin_amdgcn_s_waitcnt(0xC07F);
-    i8_epilogue<T, EPI, 1, RAGGED>(sum, reg, s_vec, res, out, M, N, m0 + wave * 32, n0, wave * 32, 0, lane);
+    const int fo = (wave >> 1) * 32, ro = (wave & 1) * 32;
+    i8_epilogue<T, EPI, 1, RAGGED, 1>(sum, reg, s_vec, res, out, M, N, m0 + ro, n0 + fo, ro, fo, lane);
 }
 
 template <typename T, int EPI, bool RAGGED, int TM>
