@@ -311,13 +311,19 @@ def rs_quantize_rows(x, q, scale, stream=None) -> None:
     assert q.stride(1) == 1 or K == 1, "the channels of a row must be contiguous"
     assert scale.is_contiguous()
     _check(lib().rs_quantize_rows(_ptr(x), M, K, x.stride(0) if M > 1 else max(K, x.stride(0)), dtype_code(x.dtype), _ptr(q),
-                                  _pitch8(q), _ptr(scale), _stream(stream)))
+                                  _pitch8(q, False), _ptr(scale), _stream(stream)))
 
 
-def _pitch8(q):
-    """Bytes between the rows of an int8 [M, K] tensor; a single row may say anything."""
+def _pitch8(q, whole_rows):
+    """Bytes between the rows of an int8 [M, K] tensor.  The kernels touch a row up to a multiple of 16 bytes (whole_rows: up to the
+    pitch): the last row has to have them too."""
     M, K = q.shape
-    return q.stride(0) if M > 1 else max(q.stride(0), (K + 15) // 16 * 16) // 16 * 16
+    if M <= 1 and K % 16 == 0:
+        return K                         # one whole row, whatever its stride says
+    pitch = q.stride(0)
+    end = q.storage_offset() + (M - 1) * pitch + (pitch if whole_rows else (K + 15) // 16 * 16)
+    assert M == 0 or (pitch == K and K % 16 == 0) or end <= q.untyped_storage().nbytes(), "no room behind the last row"
+    return pitch
 
 
 def rs_quantize_columns(w, q, scale, stream=None) -> None:
@@ -356,7 +362,7 @@ def rs_linear_i8_fwd(a, a_scale, w, w_scale, bias, res, out, epi=RS_EPI_BIAS, st
     assert w.numel() * w.element_size() >= rs_packed_linear_i8_size(K, N), "w is not packed for this K and N"
     assert bias is None or (bias.numel() == N and bias.dtype == out.dtype and bias.is_contiguous())
     assert res is None or (res.shape == out.shape and res.dtype == out.dtype and res.is_contiguous())
-    _check(lib().rs_linear_i8_fwd(_ptr(a), _pitch8(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(res), _ptr(out),
+    _check(lib().rs_linear_i8_fwd(_ptr(a), _pitch8(a, True), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(res), _ptr(out),
                                   M, N, K, epi, dtype_code(out.dtype), _stream(stream)))
 
 
@@ -379,18 +385,35 @@ def make_residual_norm_weights(w: dict) -> RsResidualNormWeights:
     return s
 
 
+def _check_vectors(cfg: RsResidualNormCfg, weights: RsResidualNormWeights) -> None:
+    """Types and sizes of the vectors that make_residual_norm_weights has kept (a structure filled by hand has none)."""
+    for (name, _), t in zip(RsResidualNormWeights._fields_, getattr(weights, "tensors", ())):
+        if t is None:
+            continue
+        stride = {"gate": cfg.gate_stride, "mod_scale": cfg.mod_stride, "mod_shift": cfg.mod_stride}.get(name, 0)
+        assert dtype_code(t.dtype) == cfg.dtype, "%s is not of the configuration's type" % name
+        assert t.shape[-1] == cfg.D and t.dim() <= 2, "%s is [D] or [B, D]" % name
+        many = t.dim() == 2 and t.shape[0] > 1
+        assert not many or (t.shape[0] == cfg.B and t.stride(0) == stride), "%s: a row for each image, its stride apart" % name
+        assert many or stride == 0 or cfg.B <= 1, "%s: one vector for all images has stride 0" % name
+
+
 def rs_residual_norm_fwd(cfg: RsResidualNormCfg, weights: RsResidualNormWeights, x, f, y, u, u_q=None, u_scale=None,
                          stream=None) -> None:
     """y = x_scale x + f_scale gate Norm_post(f), u = Norm_pre(y) (1 + mod_scale) + mod_shift; x, f, y, u: [B, N, D] (f, y, u may
     be None), u_q int8 [B * N, D] in rows a multiple of 16 bytes apart with u_scale float [B * N], or None."""
     numel = cfg.B * cfg.N * cfg.D
+    key = bytes(cfg)
+    if getattr(weights, "checked", None) != key:             # once for a configuration
+        _check_vectors(cfg, weights)
+        weights.checked = key
     _here(x, f, y, u, u_q, u_scale)
     for t in (x, f, y, u):
         assert t is None or (t.numel() == numel and t.is_contiguous() and dtype_code(t.dtype) == cfg.dtype)
     assert u_q is None or (u_q.shape == (cfg.B * cfg.N, cfg.D) and u_q.dtype == torch.int8 and u_q.stride(1) == 1)
     assert u_scale is None or (u_scale.numel() == cfg.B * cfg.N and u_scale.dtype == torch.float32 and u_scale.is_contiguous())
     _check(lib().rs_residual_norm_fwd(ctypes.byref(cfg), ctypes.byref(weights), _ptr(x), _ptr(f), _ptr(y), _ptr(u), _ptr(u_q),
-                                      0 if u_q is None else _pitch8(u_q), _ptr(u_scale), _stream(stream)))
+                                      0 if u_q is None else _pitch8(u_q, False), _ptr(u_scale), _stream(stream)))
 
 
 def rs_packed_weights_size(cfg: RsBlockCfg) -> int:

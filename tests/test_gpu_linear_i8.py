@@ -310,3 +310,22 @@ def test_two_streams_at_once():
             rs.rs_linear_i8_fwd(x[0], x[1], pw, x[3], x[4], None, o, rs.RS_EPI_BIAS_GELU, s)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(alone, outs))
+
+
+def test_rows_that_have_no_room_for_their_last_bytes_are_refused():
+    """A row of 100 bytes is written up to byte 112: not into what lies behind it."""
+    x, scale = torch.randn(3, 100, device="cuda"), torch.empty(3, device="cuda")
+    tight = torch.full((5, 100), 55, dtype=torch.int8, device="cuda")
+    for rows in (3, 1):
+        with pytest.raises((rs.RsError, AssertionError)):
+            rs.rs_quantize_rows(x[:rows], tight[:rows], scale[:rows])
+    last = torch.full((2 * 112 + 100,), 55, dtype=torch.int8, device="cuda").as_strided((3, 100), (112, 1))
+    with pytest.raises(AssertionError, match="room"):
+        rs.rs_quantize_rows(x, last, scale)
+    pw = packed(torch.ones(100, 8, dtype=torch.int8, device="cuda"))
+    with pytest.raises(AssertionError, match="room"):
+        rs.rs_linear_i8_fwd(last, scale, pw, torch.ones(8, device="cuda"), None, None, torch.empty(3, 8, device="cuda"))
+    torch.cuda.synchronize()
+    assert bool((tight == 55).all()) and bool((last == 55).all())
+    one = torch.empty(112, dtype=torch.int8, device="cuda")       # a single row: any stride will do where it is whole
+    rs.rs_quantize_rows(torch.randn(1, 112, device="cuda"), one.as_strided((1, 112), (1, 1)), scale[:1])

@@ -217,3 +217,20 @@ def test_every_number_of_lanes(rows, D):
     within(y, ry, ey, "bf16")
     within(u, ru, eu, "bf16")
     check8(u_q, u_s, ru, eu, D)
+
+
+def test_vectors_that_do_not_fit_the_configuration_are_refused():
+    B, N, D = 3, 4, 64
+    x, f, v, stride = make(B, N, D, "bf16", True, seed=2)
+    y = torch.empty_like(x)
+    ok = dict(post=rs.RS_NORM_LAYER, pre=rs.RS_NORM_NONE, gate_stride=stride, mod_stride=stride)
+    v["pre_g"] = v["pre_b"] = None
+    call = lambda v, **kw: rs.rs_residual_norm_fwd(rs.make_residual_norm_cfg(B, N, D, torch.bfloat16, **{**ok, **kw}),  # noqa: E731
+                                                   rs.make_residual_norm_weights(v), x, f, y, None)
+    call(v)
+    for bad in (dict(v, gate=v["gate"][:2]), dict(v, gate=v["gate"][:, :56]), dict(v, post_g=v["post_g"][:32]), dict(v, gate=v["gate"][0]),
+                {n: None if t is None else t.float() for n, t in v.items()}):
+        with pytest.raises(AssertionError):
+            call(bad)
+    with pytest.raises(AssertionError):
+        call(v, gate_stride=0)
