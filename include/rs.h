@@ -105,8 +105,9 @@ typedef struct {
  * (static storage, never NULL). */
 RS_API const char *rs_last_error(void);
 
-/* Library version as major*10000 + minor*100 + patch.  Buffers that rs_pack_weights has written are valid for the
- * version that wrote them and must be packed again for another one (400: fragments in place of rows). */
+/* Library version as major*10000 + minor*100 + patch.  Buffers that rs_pack_weights and rs_pack_linear_i8 have written are valid for
+ * the version that wrote them and must be packed again for another one (400: fragments in place of rows; 500: the 8-bit linear
+ * layers and rs_residual_norm_fwd). */
 RS_API int32_t rs_version(void);
 
 /* Host string (static storage): the tile configurations the matrix kernels were built with.
@@ -125,7 +126,8 @@ RS_API rs_status rs_tune_gemm_variant(int32_t variant);
  * for the recorded events (host synchronisation), adds the elapsed milliseconds and the
  * launch counts per kernel class into ms_out[RS_PROFILE_CLASSES] and
  * launches_out[RS_PROFILE_CLASSES] (host arrays), and forgets the records.
- * Classes, by index: see rs_profile_class_name (host string, static storage).
+ * Classes, by index: see rs_profile_class_name (host string, static storage).  The 8-bit layers and the quantization of
+ * their rows count as "linear", the quantization and packing of weights as "pack_weights", rs_residual_norm_fwd as "layernorm".
  */
 #define RS_PROFILE_CLASSES 11
 RS_API rs_status rs_profile_enable(int32_t enable);
@@ -286,7 +288,7 @@ RS_API rs_status rs_linear_fwd(const void *a, const void *w, const void *bias, c
  * rs_quantize_columns does the same to the columns of a weight matrix w [K, N] (fp32 or bf16): q [K, N], scale [N].
  * rs_pack_linear_i8 lays weights q [K, N] (any int8 values) out as the kernels read them: rs_packed_linear_i8_size(K, N) bytes
  *   (0 for sizes that rs_linear_i8_fwd refuses), every one of them written.  Layout of this library version, as rs_pack_weights.
- * rs_linear_i8_fwd:
+ * rs_linear_i8_fwd:  (K <= 131071: sums of that many products of 8-bit integers stay below 2^31)
  *   a : int8 (m, k) at m * lda + k, lda >= K and a multiple of 16; all M rows have lda bytes of memory.  Bytes behind column K
  *       may hold anything.        a_scale : float [M].       w : packed weights.      w_scale : float [N].
  *   bias : [N] or NULL;  res : [M, N] for RS_EPI_BIAS_RES;  out : [M, N], all in `dtype`.  out may be res; it must not overlap

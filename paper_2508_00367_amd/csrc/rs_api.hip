@@ -229,7 +229,7 @@ extern "C" {
 
 const char* rs_last_error(void) { return g_err; }
 
-int32_t rs_version(void) { return 400; }
+int32_t rs_version(void) { return 500; }
 
 const char* rs_build_info(void) { return gemm_build_info(); }
 
@@ -591,7 +591,7 @@ rs_status rs_linear_fwd(const void* a, const void* w, const void* bias, const vo
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 // Bytes from the first to the last element of `rows` rows of `width` bytes, `pitch` bytes apart.
 static size_t span(int64_t rows, int64_t pitch, int64_t width) { return rows > 0 ? (size_t)((rows - 1) * pitch + width) : 0; }
-// A row pitch of at most 2^31 - 1 elements: spans of 2^31 rows stay below 2^63 bytes.
+// Spans of 2^31 rows of fp32 that far apart stay below 2^63 bytes.
 constexpr int64_t kMaxPitch = ((int64_t)1 << 29) - 1;
 
 rs_status rs_quantize_rows(const void* x, int64_t M, int32_t K, int64_t ldx, rs_dtype dtype, int8_t* q, int64_t ldq, float* scale,
