@@ -201,11 +201,13 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const E
 // straight into the registers of the one wave that needs them, the activations through a ring of four LDS stages of 128 k, copied
 // three slices ahead, as in gemm_bf16_direct_kernel, whose slices hold as many bytes.  TM = 8, one workgroup per CU with 256
 // accumulator registers a lane: the weights of a slice serve twice the rows.
-// What bounds the large layers is the power the chip may draw: 32768 x 4096 -> 4096 runs at 1.6 GHz with the matrix cores busy 73 % of the
-// cycles, and a layer's time is the sum of what its products and its bytes cost (50432 x K -> 2304: 42 us + 0.088 us per k, 2.6 POPS; stores and
-// loads overlap in time but not in power; starting the second workgroup of a CU half a tile later changes nothing).  So the
-// kernel with the fewest bytes moved per product wins where it fills the chip.  (256 x 256 with waves of 128 x 128, half the LDS
-// reads but weights loaded by two waves each: 8192^3 423 -> 447 us.)
+// What bounds the large layers is power first: 32768 x 4096 -> 4096 runs at 1.7 GHz with the matrix cores busy 70 % of the cycles (2.45
+// POPS; a loop of nothing but these matrix instructions reaches 4.3), and a layer's time is the sum of what its products and its
+// bytes cost (50432 x K -> 2304: 42 us + 0.088 us per k; stores and loads overlap in time but not in power; starting the second workgroup
+// of a CU half a tile later changes nothing).  So the kernel with the fewest bytes moved per product wins where it fills the chip.
+// 8192^3: 420 us, without the copies in the loop 390, without the weight loads 392, without both 363.  No better: waves of 128 x 128 in a 256 x 256
+// tile (half the LDS reads, weights loaded by two waves each) 447; weights two slices ahead 429; the slices of neighbouring row
+// panels in rotated order, for layers whose weights all panels read at once (no change).
 // ---------------------------------------------------------------------------
 template <typename T, int EPI, bool RAGGED, int TM>
 __global__ __launch_bounds__(256, TM == 8 ? 1 : 2) void gemm_i8_direct_kernel(const int8_t* __restrict__ a, int lda, const float* __restrict__ a_scale,
