@@ -25,7 +25,7 @@ __device__ __forceinline__ float gelu_of(float x, const bf16raw*) { return gelu_
 // 128 bytes) per 32-row group: residual rows arrive there by direct copies, a lane picks up its 4 features and puts the result
 // back in place, the group leaves as 16 bytes per lane in whole row segments.  In bf16 a region holds the wave's 64 features, in
 // fp32 32 of them, and the features go in two passes.  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
-// anywhere (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 7).
+// anywhere; their pieces go at addresses aligned to the element (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 9.4).
 // ---------------------------------------------------------------------------
 template <typename T, int TN> struct EpiI8 {              // a wave of 32 TN features
     static constexpr int F = sizeof(T) == 4 ? 32 : 32 * TN;  // features of a region
@@ -136,7 +136,8 @@ __device__ __forceinline__ f32x4 bias4(const unsigned char* at, const float*) { 
 // `vec`: the tile's vectors (landed); row0 and f0: the wave's first row and feature inside the tile.  The regions are this wave's
 // own and consecutive 4 KB apart (one array per wave).
 template <typename T, int EPI, int TM, bool RAGGED, int TN>
-__device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const EpiRegions<TM>& reg, const unsigned char* vec, const T* res, T* out, int64_t M, int N, int64_t m_base, int n_base, int row0, int f0, int lane) {
+__device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const EpiRegions<TM>& reg, const unsigned char* vec, const T* res, T* out,
+                                            int64_t M, int N, int64_t m_base, int n_base, int row0, int f0, int lane) {
     constexpr int P = EpiI8<T, TN>::PASSES, F = EpiI8<T, TN>::F, NI = TN / P, PIECES = EpiI8<T, TN>::PIECES;
     const int l32 = lane & 31, g = lane >> 5;
     if (n_base >= N || m_base >= M) return;
@@ -707,7 +708,8 @@ static void launch_i8_part(const GemmI8Args& g, hipStream_t s) {
     }
 }
 
-// Rows in parts of at most 2^22 tiles of 128 x 64 (a launch holds fewer than 2^32 threads).
+// Rows in parts of at most 2^22 tiles of 128 x 64: 2^23 workgroups of the smallest tile that takes so many rows (a launch holds fewer than 2^32
+// threads).
 template <typename T, int EPI>
 static hipError_t launch_i8(const GemmI8Args& g, hipStream_t s) {
     const int64_t rows = ((int64_t)1 << 22) / ((g.N + 63) / 64) * 128;

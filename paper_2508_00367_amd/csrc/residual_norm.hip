@@ -2,7 +2,12 @@
 // modulation in front of the next branch, whose rows may leave in 8 bits:
 //   y = x_scale x + f_scale gate . Norm_post(f),   u = Norm_pre(y) . (1 + mod_scale) + mod_shift
 // A row's f, then y, then u stay in registers between the steps; y goes into the second norm as it is in fp32, unrounded.
-// Variances are taken over the deviations from the mean.  Bound by reading x and f and writing y and u once.
+// Variances are taken over the deviations from the mean.
+// Bound by reading x and f and writing y and u once, at the rate of a copy (5.1 TB/s): 4 x 4097 x 1024 fp32 with every vector 51 us, 5.3 TB/s; 256 x
+// 197 x 768 bf16 with one norm 56 us, 5.5 TB/s; with two norms and 8-bit rows (a third of the stores) 61-68 us, 4.0-4.4 TB/s: about 40 ALU instructions
+// a value then.  What it took: x and f requested together before anything is summed; every lane with work (below); vectors
+// through resources, whose scalar addresses leave the registers to the rows (161 -> 125, four waves per SIMD; forced lower, they spill: 107 us); fp32 in
+// pieces of 4 channels, so that neighbouring lanes' pieces lie side by side (58 -> 51); stores through the L2 (60 -> 56).
 #include "quantize.hpp"
 
 namespace rs {
@@ -194,7 +199,9 @@ static hipError_t go(const ResidualNormArgs& p, hipStream_t s) {
 }
 
 // The fewest lanes that hold a row in up to four pieces each: every lane busy at 192, 384 and 768 channels, where a wave per row
-// leaves a quarter to five eighths of its lanes without work.
+// leaves a quarter to five eighths of its lanes without work (512 x 197 x 192 bf16 79 -> 34 us, 256 x 197 x 768 97 -> 61).
+// Where rows are too few to fill the chip so, one piece per lane: the way through is shorter.  Two LayerNorms, us, four pieces / one: 512
+// channels at 1 row 5.2 / 3.4, at 2000 6.6 / 4.5; 256 at 4000 6.5 / 4.6; 1024 at 197 6.1 / 4.4, at 1000 6.6 / 6.0.
 template <typename T>
 static hipError_t launch_rn(const ResidualNormArgs& p, hipStream_t s) {
     const int n = p.D / kE<T>;
