@@ -24,7 +24,8 @@ __device__ __forceinline__ float gelu_of(float x, const bf16raw*) { return gelu_
 // 32 i + 8 q + 4 g + e in register 4 q + e of acc[i][j].  Only the traffic with memory goes through LDS, one 4 KB region (32 rows of
 // 128 bytes) per 32-row group: residual rows arrive there by direct copies, a lane picks up its 4 features and puts the result
 // back in place, the group leaves as 16 bytes per lane in whole row segments.  In bf16 a region holds the wave's 64 features, in
-// fp32 32 of them, and the features go in two passes.  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
+// fp32 32 of them, and a group goes in two passes.  Rows that are whole lines are written through the L2 (store16_wt); of others a line is
+// written in parts, which only the L2 can join (fp32 43814 x 128 -> 6228 555 us written through, pass by pass; so 330).  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
 // anywhere; their pieces go at addresses aligned to the element (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 9.4).
 // ---------------------------------------------------------------------------
 template <typename T, int TN> struct EpiI8 {              // a wave of 32 TN features
@@ -84,29 +85,25 @@ __device__ __forceinline__ void store_piece(T* row, int c, int n, u32x4 v) {
         if (c * E + i < n) row[c * E + i] = w.e[i];
 }
 
-// Residual rows of one pass into the regions; rows past M read as zeros, pieces past N are of the next row and not used.
-template <typename T, int TM, bool RAGGED, int F>
-__device__ __forceinline__ void i8_request_res(const EpiRegions<TM>& reg, const T* res, int64_t M, int N, int64_t m_base, int n,
-                                               int lane) {
-    const int64_t left = M - m_base;
-    if (n >= N || left <= 0) return;
-    const int rows = (int)(left < 32 * TM ? left : 32 * TM);
-    const T* base = res + m_base * N + n;
+// F features from n on of 32 residual rows into a region; rows past M read as zeros (or stay what they are), pieces past N are of the
+// next row and not used.
+template <typename T, bool RAGGED, int F>
+__device__ __forceinline__ void i8_request_res(unsigned char* region, const T* res, int64_t M, int N, int64_t m, int n, int lane) {
+    const int rows = (int)min(M - m, (int64_t)32);
+    if (n >= N || rows <= 0) return;
+    const T* base = res + m * N + n;
     if constexpr (RAGGED) {
 #pragma unroll
-        for (int p = 0; p < 4 * TM; ++p) {
+        for (int p = 0; p < 4; ++p) {
             const int r = p * 8 + (lane >> 3), c = lane & 7;
-            if (r < rows) *reinterpret_cast<u32x4*>(reg.r[p >> 2] + (r & 31) * 128 + ((c ^ epi_swz(r & 31)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
+            if (r < rows) *reinterpret_cast<u32x4*>(region + r * 128 + ((c ^ epi_swz(r)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
         }
     } else {
-        const int64_t bytes = ((int64_t)(rows - 1) * N + min(N - n, F)) * (int)sizeof(T);
-        const __amdgpu_buffer_rsrc_t rs_res = make_rsrc(base, bytes);
+        const __amdgpu_buffer_rsrc_t rs_res = make_rsrc(base, ((int64_t)(rows - 1) * N + min(N - n, F)) * (int)sizeof(T));
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             const int r = p * 8 + (lane >> 3);
-            const int voff = r * N * (int)sizeof(T) + (((lane & 7) ^ epi_swz(r)) << 4);
-#pragma unroll
-            for (int j = 0; j < TM; ++j) dma16(rs_res, reg.r[j] + p * 1024, voff, j * 32 * N * (int)sizeof(T));
+            dma16(rs_res, region + p * 1024, r * N * (int)sizeof(T) + (((lane & 7) ^ epi_swz(r)) << 4), 0);
         }
     }
 }
@@ -145,55 +142,75 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const E
 #pragma unroll
     for (int j = 0; j < TM; ++j) as[j] = *reinterpret_cast<const float*>(vec + kVecRows + (row0 + j * 32 + l32) * 4);
     const int rows = (int)(M - m_base < 32 * TM ? M - m_base : 32 * TM);
+    const bool lines = (int64_t)N * sizeof(T) % 128 == 0;
+    f32x4 ws[TN][4], bv[TN][4];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const int n = n_base + p * F;
-        if (n >= N) break;
-        if (EPI == EPI_BIAS_RES) {
-            if (p > 0) __builtin_amdgcn_s_waitcnt(0xC07F);  // what the last pass reads from the regions has been read
-            i8_request_res<T, TM, RAGGED, F>(reg, res, M, N, m_base, n, lane);
-            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & 0xC07F);  // every residual row of the pass has landed
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int f = f0 + i * 32 + q * 8 + g * 4;
+            ws[i][q] = *reinterpret_cast<const f32x4*>(vec + f * 4);
+            bv[i][q] = bias4(vec + kVecBias + f * (int)sizeof(T), (const T*)nullptr);
         }
-        f32x4 ws[NI][4], bv[NI][4];
+    // 32-row group j, features p F .. of the wave's, through the region at buf
+    auto group = [&](int p, int j, unsigned char* buf) {
+        const int n = n_base + p * F;
+        if (n >= N) return;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int f = f0 + p * F + i * 32 + q * 8 + g * 4;
-                ws[i][q] = *reinterpret_cast<const f32x4*>(vec + f * 4);
-                bv[i][q] = bias4(vec + kVecBias + f * (int)sizeof(T), (const T*)nullptr);
+                unsigned char* at = buf + region_at<T>(l32, i * 32 + q * 8 + g * 4);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int fi = P > 1 ? p : i;
+                    v[e] = fmaf((float)acc[fi][j][4 * q + e], as[j] * ws[fi][q][e], bv[fi][q][e]);
+                    if (EPI == EPI_BIAS_GELU) v[e] = gelu_of(v[e], (const T*)nullptr);
+                }
+                if (EPI == EPI_BIAS_RES) res_add(v, at, (const T*)nullptr);
+                put4(at, v, (T*)nullptr);  // in place: this lane alone reads and writes these bytes
             }
+        // the group leaves (LDS accesses of one wave are served in order)
         const __amdgpu_buffer_rsrc_t rs_out = make_rsrc(out + m_base * N + n, ((int64_t)(rows - 1) * N + min(N - n, F)) * (int)sizeof(T));
 #pragma unroll
-        for (int j = 0; j < TM; ++j) {
-            unsigned char* buf = reg.r[j];
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    unsigned char* at = buf + region_at<T>(l32, i * 32 + q * 8 + g * 4);
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = fmaf((float)acc[P > 1 ? p : i][j][4 * q + e], as[j] * ws[i][q][e], bv[i][q][e]);
-                        if (EPI == EPI_BIAS_GELU) v[e] = gelu_of(v[e], (const T*)nullptr);
-                    }
-                    if (EPI == EPI_BIAS_RES) res_add(v, at, (const T*)nullptr);
-                    put4(at, v, (T*)nullptr);  // in place: this lane alone reads and writes these bytes
-                }
-            // the group leaves (LDS accesses of one wave are served in order)
-#pragma unroll
-            for (int s = 0; s < PIECES / 2; ++s) {
-                const int r = s * (64 / PIECES) + lane / PIECES, c = lane % PIECES;
-                const u32x4 o4 = *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4));
-                if constexpr (RAGGED) {
-                    if (j * 32 + r < rows) store_piece(out + (m_base + j * 32 + r) * N + n, c, N - n, o4);
-                } else {
-                    const bool in = j * 32 + r < rows && n + c * (16 / (int)sizeof(T)) < N;
-                    store16_wt(rs_out, in ? ((j * 32 + r) * N) * (int)sizeof(T) + c * 16 : kPastEnd, o4);
-                }
+        for (int s = 0; s < PIECES / 2; ++s) {
+            const int r = s * (64 / PIECES) + lane / PIECES, c = lane % PIECES;
+            const u32x4 o4 = *reinterpret_cast<const u32x4*>(buf + r * 128 + ((c ^ epi_swz(r)) << 4));
+            if constexpr (RAGGED) {
+                if (j * 32 + r < rows) store_piece(out + (m_base + j * 32 + r) * N + n, c, N - n, o4);
+            } else {
+                const bool in = j * 32 + r < rows && n + c * (16 / (int)sizeof(T)) < N;
+                const int at = in ? ((j * 32 + r) * N) * (int)sizeof(T) + c * 16 : kPastEnd;
+                if (lines) store16_wt(rs_out, at, o4);
+                else __builtin_amdgcn_raw_buffer_store_b128(o4, rs_out, at, 0, 0);
             }
         }
+    };
+    if (P > 1 && EPI != EPI_BIAS_RES && !RAGGED && lines) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) group(p, j, reg.r[j]);
+        return;
+    }
+    // A row's passes one behind the other, so that a line they share is written at about one time (rows of whole lines: above, 16388 x 1024 ->
+    // 4096 106 -> 102 us).  With a residual TM / P groups at a time, each pass in a region of its own.
+    constexpr int GROUPS = EPI == EPI_BIAS_RES ? TM / P : TM;
+#pragma unroll
+    for (int j0 = 0; j0 < TM; j0 += GROUPS) {
+        if constexpr (EPI == EPI_BIAS_RES) {
+            if (j0 > 0) __builtin_amdgcn_s_waitcnt(0xC07F);  // what the last groups read from the regions has been read
+#pragma unroll
+            for (int j = 0; j < GROUPS; ++j)
+#pragma unroll
+                for (int p = 0; p < P; ++p) i8_request_res<T, RAGGED, F>(reg.r[j * P + p], res, M, N, m_base + (j0 + j) * 32, n_base + p * F, lane);
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0) & 0xC07F);  // all of them have landed
+        }
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j)
+#pragma unroll
+            for (int p = 0; p < P; ++p) group(p, j0 + j, reg.r[EPI == EPI_BIAS_RES ? j * P + p : j]);
     }
 }
 
