@@ -7,7 +7,8 @@
 // 197 x 768 bf16 with one norm 56 us, 5.5 TB/s; with two norms and 8-bit rows (a third of the stores) 61-68 us, 4.0-4.4 TB/s: about 40 ALU instructions
 // a value then.  What it took: x and f requested together before anything is summed; every lane with work (below); vectors
 // through resources, whose scalar addresses leave the registers to the rows (161 -> 125, four waves per SIMD; forced lower, they spill: 107 us); fp32 in
-// pieces of 4 channels, so that neighbouring lanes' pieces lie side by side (58 -> 51); stores through the L2 (60 -> 56).
+// pieces of 4 channels, so that neighbouring lanes' pieces lie side by side (58 -> 51); stores through the L2 (60 -> 56) where rows are whole lines,
+// and left to the L2 to join where they are not (8 x 4097 x 4040 fp32 474 -> 389, x 1000 bf16 65 -> 60).
 #include "quantize.hpp"
 
 namespace rs {
@@ -74,7 +75,7 @@ __device__ __forceinline__ void row_norm(float (&v)[P][E], rs_norm kind, float e
 
 // G lanes per row (8 .. 64, or a workgroup of 256 .. 1024), P pieces per lane: lane l has pieces l, l + G, ...
 // The rows of a wave are neighbours: one resource holds them, and what lies past the last row or the end of a row is aimed
-// past its end.  Outputs are written through the L2 (store16_wt).
+// past its end.
 template <typename T, int G, int P>
 __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(ResidualNormArgs p) {
     __shared__ float s_red[G > 64 ? G / 64 : 1];
@@ -82,6 +83,11 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
     constexpr int ES = sizeof(T), E = kE<T>;
     const int D = p.D, n = D / E, sub = threadIdx.x % G;
     const float inv_d = 1.0f / (float)D;
+    const bool lines = D * ES % 128 == 0;
+    auto put = [&](__amdgpu_buffer_rsrc_t r, int at, u32x4 v) {
+        if (lines) store16_wt(r, at, v);
+        else __builtin_amdgcn_raw_buffer_store_b128(v, r, at, 0, 0);
+    };
     const int64_t wave0 = (int64_t)blockIdx.x * RPB + (G > 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPW);
     for (int64_t row0 = wave0; row0 < p.rows; row0 += (int64_t)gridDim.x * RPB) {
         const int my = G < 64 ? (threadIdx.x & 63) / G : 0;
@@ -143,7 +149,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
         for (int c = 0; c < P; ++c) {
 #pragma unroll
             for (int i = 0; i < E; ++i) v[c][i] = sub + c * G < n ? fmaf(p.x_scale, at<T>(rx[c], i), p.f_scale * v[c][i]) : 0.f;
-            if (p.y) store16_wt(rs_y, off[c], piece<T>(v[c]));
+            if (p.y) put(rs_y, off[c], piece<T>(v[c]));
         }
         if (!p.u && !p.u_q) continue;
         RS_VEC(va, pre_g);
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
 #undef RS_VEC_MOD
         if (p.u) {
 #pragma unroll
-            for (int c = 0; c < P; ++c) store16_wt(rs_u, off[c], piece<T>(v[c]));
+            for (int c = 0; c < P; ++c) put(rs_u, off[c], piece<T>(v[c]));
         }
         if (p.u_q) {
             float amax = 0.f;
