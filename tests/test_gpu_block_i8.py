@@ -107,7 +107,7 @@ def test_each_step_of_a_block(B, N, D, H, Dm, P, K, dtype, norm, post):
 
 
 def test_near_the_block_in_full_precision():
-    """The 8-bit block against the fp64 checker's block: every operand of the four products is off by at most half of 1/127 of its row's or
+    """The 8-bit block against the fp64 oracle's block: every operand of the four products is off by at most half of 1/127 of its row's or
     column's largest value, 0.29 of a step rms; rows of unit normals reach 3.5 of their standard deviation, so that is 0.8 % of an
     operand, and 1.1 % of a product of two, for a branch of two layers (and softmax or GELU, of slope 1.13 at most, between them) 1.8 %.
     Twice that, relative in the 2-norm, for the two branches and the residual stream that carries the first into the second."""
