@@ -134,6 +134,15 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
                 v[c][i] = (expr_);                                                                        \
             }                                                                                             \
     }
+// v . g + b, each where there is one
+#define RS_AFFINE(g_, b_)                                                                                 \
+    if (g_ && b_) {                                                                                       \
+        _Pragma("unroll") for (int c = 0; c < P; ++c)                                                     \
+            _Pragma("unroll") for (int i = 0; i < E; ++i) v[c][i] = fmaf(v[c][i], at<T>(va[c], i), at<T>(vb[c], i)); \
+    } else {                                                                                              \
+        RS_EACH(g_, va, v[c][i] * t)                                                                      \
+        RS_EACH(b_, vb, v[c][i] + t)                                                                      \
+    }
         RS_VEC(va, post_g);
         RS_VEC(vb, post_b);
         RS_VEC_GATE(vc);
@@ -142,8 +151,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
 #pragma unroll
             for (int i = 0; i < E; ++i) v[c][i] = at<T>(w[c], i);
         row_norm<G, P, E>(v, p.post, p.post_eps, inv_d, n, sub, s_red);
-        RS_EACH(p.post_g, va, v[c][i] * t)
-        RS_EACH(p.post_b, vb, v[c][i] + t)
+        RS_AFFINE(p.post_g, p.post_b)
         RS_EACH(p.gate, vc, v[c][i] * t)
 #pragma unroll
         for (int c = 0; c < P; ++c) {
@@ -157,11 +165,11 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
         RS_VEC_MOD(vc, mod_scale);
         RS_VEC_MOD(vd, mod_shift);
         row_norm<G, P, E>(v, p.pre, p.pre_eps, inv_d, n, sub, s_red);
-        RS_EACH(p.pre_g, va, v[c][i] * t)
-        RS_EACH(p.pre_b, vb, v[c][i] + t)
+        RS_AFFINE(p.pre_g, p.pre_b)
         RS_EACH(p.mod_scale, vc, fmaf(v[c][i], t, v[c][i]))
         RS_EACH(p.mod_shift, vd, v[c][i] + t)
 #undef RS_EACH
+#undef RS_AFFINE
 #undef RS_VEC
 #undef RS_VEC_GATE
 #undef RS_VEC_MOD
