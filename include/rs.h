@@ -277,7 +277,8 @@ RS_API rs_status rs_linear_fwd(const void *a, const void *w, const void *bias, c
  * Linear layers in 8-bit integers (W8A8): integers with one scale for each token (row of the activations) and each output channel
  * (column of the weights),
  *     out[m, n] = epilogue( (sum_k a[m, k] w[k, n]) * a_scale[m] * w_scale[n] + bias[n] )
- * the sum exact in 32-bit integers, all behind it in fp32, rounded to the output type once.  Epilogues as in rs_linear_fwd.
+ * the sum exact in 32-bit integers, all behind it in fp32, rounded to the output type once.  Epilogues as in rs_linear_fwd; GELU in bf16
+ * is off by less than that rounding wherever it is 1e-18 or more.
  *
  * rs_quantize_rows forms 8-bit rows from fp32 or bf16 ones, symmetric about zero:
  *     scale[m] = max(max_k |x[m, k]| * (1 / 127), FLT_MIN),   q[m, k] = round(x[m, k] * (1 / scale[m]))
