@@ -53,6 +53,7 @@ class RsBlockCfg(ctypes.Structure):
 
 class RsResidualNormWeights(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("post_g", "post_b", "gate", "pre_g", "pre_b", "mod_scale", "mod_shift")]
+    device = None  # of the tensors that make_residual_norm_weights has kept
 
 
 class RsResidualNormCfg(ctypes.Structure):
@@ -397,6 +398,7 @@ def make_residual_norm_weights(w: dict) -> RsResidualNormWeights:
     assert len({t.dtype for t in s.tensors if t is not None}) <= 1, "the vectors must be of one type"
     for name, _ in RsResidualNormWeights._fields_:
         setattr(s, name, _ptr(w.get(name)))
+    s.device = next((t.get_device() for t in s.tensors if t is not None), None)
     return s
 
 
@@ -424,6 +426,7 @@ def rs_residual_norm_fwd(cfg: RsResidualNormCfg, weights: RsResidualNormWeights,
         seen = weights.seen = (key, cfg.B * cfg.N, cfg.D, torch.float32 if cfg.dtype == RS_F32 else torch.bfloat16)
     _, rows, D, dt = seen
     _here(x, f, y, u, u_q, u_scale)
+    assert weights.device is None or weights.device == x.get_device(), "the vectors are on another device"
     ptrs = []
     for t in (x, f, y, u):
         if t is not None:
