@@ -104,10 +104,11 @@ __device__ __forceinline__ void store_piece(T* row, int c, int n, u32x4 v) {
         if (c * E + i < n) row[c * E + i] = w.e[i];
 }
 
-// F features from n on of 32 residual rows into a region; rows past M read as zeros (or stay what they are), pieces past N are of the
-// next row and not used.
+// F features from n on of 32 residual rows into a region, and no more: the next ones are another wave's, which may be writing them by now (out
+// may be res).  Rows past M read as zeros (or stay what they are), pieces past N are of the next row and not used.
 template <typename T, bool RAGGED, int F>
 __device__ __forceinline__ void i8_request_res(unsigned char* region, const T* res, int64_t M, int N, int64_t m, int n, int lane) {
+    constexpr int PIECES = F * (int)sizeof(T) / 16;
     const int rows = (int)min(M - m, (int64_t)32);
     if (n >= N || rows <= 0) return;
     const T* base = res + m * N + n;
@@ -115,14 +116,14 @@ __device__ __forceinline__ void i8_request_res(unsigned char* region, const T* r
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             const int r = p * 8 + (lane >> 3), c = lane & 7;
-            if (r < rows) *reinterpret_cast<u32x4*>(region + r * 128 + ((c ^ epi_swz(r)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
+            if (r < rows && c < PIECES) *reinterpret_cast<u32x4*>(region + r * 128 + ((c ^ epi_swz(r)) << 4)) = load_piece(base + (int64_t)r * N, c, N - n);
         }
     } else {
         const __amdgpu_buffer_rsrc_t rs_res = make_rsrc(base, ((int64_t)(rows - 1) * N + min(N - n, F)) * (int)sizeof(T));
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const int r = p * 8 + (lane >> 3);
-            dma16(rs_res, region + p * 1024, r * N * (int)sizeof(T) + (((lane & 7) ^ epi_swz(r)) << 4), 0);
+            const int r = p * 8 + (lane >> 3), c = (lane & 7) ^ epi_swz(r);
+            dma16(rs_res, region + p * 1024, c < PIECES ? r * N * (int)sizeof(T) + (c << 4) : kPastEnd, 0);
         }
     }
 }
