@@ -43,8 +43,9 @@ __device__ __forceinline__ float gelu_of(float x, const bf16raw*) { return gelu_
 // 32 i + 8 q + 4 g + e in register 4 q + e of acc[i][j].  Only the traffic with memory goes through LDS, one 4 KB region (32 rows of
 // 128 bytes) per 32-row group: residual rows arrive there by direct copies, a lane picks up its 4 features and puts the result
 // back in place, the group leaves as 16 bytes per lane in whole row segments.  In bf16 a region holds the wave's 64 features, in
-// fp32 32 of them, and a group goes in two passes.  Rows that are whole lines are written through the L2 (store16_wt); of others a line is
-// written in parts, which only the L2 can join (fp32 43814 x 128 -> 6228 555 us written through, pass by pass; so 330).  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
+// fp32 32 of them, and a group goes in two passes.  Waves that store whole lines do so through the L2 (store16_wt); of other rows, and of half-filled
+// regions, a line is written in parts, which only the L2 can join (fp32 43814 x 128 -> 6228 555 us written through, pass by pass; so 330.  Half-filled
+// regions: the same either way, 788 x 768 -> 768 4.2 us, 50432 x 768 -> 64 12.0).  RAGGED: rows of `out` are no whole 16-byte pieces, so that they start
 // anywhere; their pieces go at addresses aligned to the element (2013 x 64 -> 1356 with residual an element per lane 18.9 us, so 9.4).
 // ---------------------------------------------------------------------------
 template <typename T, int TN> struct EpiI8 {              // a wave of 32 TN features
@@ -162,7 +163,7 @@ __device__ __forceinline__ void i8_epilogue(const i32x16 (&acc)[TN][TM], const E
 #pragma unroll
     for (int j = 0; j < TM; ++j) as[j] = *reinterpret_cast<const float*>(vec + kVecRows + (row0 + j * 32 + l32) * 4);
     const int rows = (int)(M - m_base < 32 * TM ? M - m_base : 32 * TM);
-    const bool lines = (int64_t)N * sizeof(T) % 128 == 0;
+    const bool lines = PIECES == 8 && (int64_t)N * sizeof(T) % 128 == 0;
     f32x4 ws[TN][4], bv[TN][4];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
