@@ -323,7 +323,7 @@ RS_API rs_status rs_linear_i8_fwd(const int8_t *a, int64_t lda, const float *a_s
  *   pre_b are [D]; gate is read at image * gate_stride, mod_scale and mod_shift at image * mod_stride (elements; 0: one
  *   vector for all images).  post_g, post_b and gate must be NULL if f is, and the two vectors of a norm if it is RS_NORM_NONE.
  * D % 8 == 0, D <= 16384, strides multiples of 8 from 0 to 2^24, B * N < 2^31, eps > 0 for a norm that is taken.  u_scale must be 4-byte
- * aligned.  No workspace.  Deterministic.
+ * aligned.  No workspace.  Deterministic; a row's results do not depend on B and N.
  */
 typedef enum { RS_NORM_NONE = 0, RS_NORM_LAYER = 1, RS_NORM_RMS = 2 } rs_norm;
 typedef struct {

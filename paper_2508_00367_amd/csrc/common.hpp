@@ -180,7 +180,8 @@ __device__ __forceinline__ float chunk_sq(const float (&v)[8], float mean, float
 // Statistics of a row a wave holds as MAXC chunks of 8 values per lane (lane l: chunks l, l + 64,
 // ...; chunks at or past nchunk hold zeros): (mean, 1 / sqrt(population variance + eps)), the
 // variance taken over the deviations from the mean.  One fixed order of additions, shared by
-// every kernel that produces LayerNorm statistics, so that they all give the same bits.
+// every kernel that produces LayerNorm statistics for a block call, so that they all give the same bits
+// (rs_residual_norm_fwd has one of its own: row_sum in residual_norm.hip).
 template <int MAXC>
 __device__ __forceinline__ float2 wave_row_stats(const float (&v)[MAXC][8], int nchunk, int lane, int D, float eps) {
     float sum = 0.f;

@@ -27,10 +27,10 @@ __device__ __forceinline__ u32x4 piece(const float (&v)[kE<T>]) {
     else return u32x4{pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7])};
 }
 
-// Sum, or the largest magnitude, over the G lanes of a row (more than 64: the waves of a workgroup, in wave order).
-template <int G, bool MAX>
-__device__ __forceinline__ float row_reduce(float v, float* s) {
-    auto op = [](float a, float b) { return MAX ? amax_step(a, b) : a + b; };
+// The largest magnitude over the G lanes of a row (more than 64: the waves of a workgroup).
+template <int G>
+__device__ __forceinline__ float row_amax(float v, float* s) {
+    auto op = [](float a, float b) { return amax_step(a, b); };
     v = lanes_reduce<(G < 64 ? G : 64)>(v, op);
     if constexpr (G > 64) {
         __syncthreads();
@@ -43,17 +43,49 @@ __device__ __forceinline__ float row_reduce(float v, float* s) {
     return v;
 }
 
+// The sum over a row of what its pieces add up to, t[c] piece lane + c G of it.  Rows of up to 256 pieces have one order of additions
+// whatever G and P are: pieces 128 apart first, then 64, and so on down to neighbours, absent ones being zeros.  So a row's bits do not depend on
+// how many rows there are, by which the lanes are chosen.  (Longer rows have one G and P each: the waves' sums are added in wave order.)
+template <int G, int P>
+__device__ __forceinline__ float row_sum(const float (&t)[P], float* s) {
+    float v = t[0];
+    if constexpr (P == 2) v = t[0] + t[1];
+    if constexpr (P == 3) v = (t[0] + t[2]) + t[1];
+    if constexpr (P == 4) v = (t[0] + t[2]) + (t[1] + t[3]);
+    if constexpr (G > 64 && P == 1) {
+        static_assert(G == 256, "four waves: 128 and 64 pieces apart");
+        const int lane = threadIdx.x & 63;
+        __syncthreads();
+        s[threadIdx.x] = v;
+        __syncthreads();
+        v = (s[lane] + s[lane + 128]) + (s[lane + 64] + s[lane + 192]);
+    }
+    v = lanes_sum<(G < 64 ? G : 64)>(v);
+    if constexpr (G > 64 && P > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = s[0];
+#pragma unroll
+        for (int i = 1; i < G / 64; ++i) v += s[i];
+    }
+    return v;
+}
+
 // v = Norm(v); pieces past the row's end (`n` of them are inside) hold zeros before and after, and the deviations leave them out.
 template <int G, int P, int E>
 __device__ __forceinline__ void row_norm(float (&v)[P][E], rs_norm kind, float eps, float inv_d, int n, int sub, float* s) {
+#pragma clang fp contract(off)  // the same operations whatever G and P are
     if (kind == RS_NORM_NONE) return;
+    float t[P];
     if (kind == RS_NORM_LAYER) {
-        float sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < P; ++c)
+        for (int c = 0; c < P; ++c) {
+            t[c] = v[c][0];
 #pragma unroll
-            for (int i = 0; i < E; ++i) sum += v[c][i];
-        const float mean = row_reduce<G, false>(sum, s) * inv_d;
+            for (int i = 1; i < E; ++i) t[c] += v[c][i];
+        }
+        const float mean = row_sum<G, P>(t, s) * inv_d;
 #pragma unroll
         for (int c = 0; c < P; ++c) {
             const float m = sub + c * G < n ? mean : 0.f;
@@ -61,12 +93,13 @@ __device__ __forceinline__ void row_norm(float (&v)[P][E], rs_norm kind, float e
             for (int i = 0; i < E; ++i) v[c][i] -= m;
         }
     }
-    float sq = 0.f;
 #pragma unroll
-    for (int c = 0; c < P; ++c)
+    for (int c = 0; c < P; ++c) {
+        t[c] = v[c][0] * v[c][0];
 #pragma unroll
-        for (int i = 0; i < E; ++i) sq = fmaf(v[c][i], v[c][i], sq);
-    const float r = rsqrtf(fmaf(row_reduce<G, false>(sq, s), inv_d, eps));
+        for (int i = 1; i < E; ++i) t[c] = fmaf(v[c][i], v[c][i], t[c]);
+    }
+    const float r = rsqrtf(fmaf(row_sum<G, P>(t, s), inv_d, eps));
 #pragma unroll
     for (int c = 0; c < P; ++c)
 #pragma unroll
@@ -78,7 +111,8 @@ __device__ __forceinline__ void row_norm(float (&v)[P][E], rs_norm kind, float e
 // past its end.
 template <typename T, int G, int P>
 __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(ResidualNormArgs p) {
-    __shared__ float s_red[G > 64 ? G / 64 : 1];
+#pragma clang fp contract(off)  // as in row_norm
+    __shared__ float s_red[G <= 64 ? 1 : P == 1 ? G : G / 64];
     constexpr int RPW = G < 64 ? 64 / G : 1, RPB = G > 64 ? 1 : 4 * RPW;  // rows of a wave, of a workgroup
     constexpr int ES = sizeof(T), E = kE<T>;
     const int D = p.D, n = D / E, sub = threadIdx.x % G;
@@ -186,7 +220,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void residual_norm_kernel(Residu
                     v[c][i] = sub + c * G < n ? v[c][i] : 0.f;
                     amax = amax_step(amax, v[c][i]);
                 }
-            const QuantScale qs = quant_scale(row_reduce<G, true>(amax, s_red));
+            const QuantScale qs = quant_scale(row_amax<G>(amax, s_red));
             const int npad = (D + 15) / 16 * 16 / E;  // zeros up to a multiple of 16
 #pragma unroll
             for (int c = 0; c < P; ++c) {
