@@ -13,7 +13,6 @@ __device__ __forceinline__ float amax_step(float a, float b) {
     const uint32_t x = __float_as_uint(a), y = __float_as_uint(b) & 0x7fffffffu;
     return __uint_as_float(x > y ? x : y);
 }
-__device__ __forceinline__ float wave_amax(float v) { return lanes_reduce<64>(v, [](float a, float b) { return amax_step(a, b); }); }
 
 struct QuantScale {
     float scale, inv;
