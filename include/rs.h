@@ -106,8 +106,8 @@ typedef struct {
 RS_API const char *rs_last_error(void);
 
 /* Library version as major*10000 + minor*100 + patch.  Buffers that rs_pack_weights and rs_pack_linear_i8 have written are valid for
- * the version that wrote them and must be packed again for another one (400: fragments in place of rows; 500: the 8-bit linear
- * layers and rs_residual_norm_fwd). */
+ * the version that wrote them and must be packed again for another one that lays them out otherwise (400: fragments in place of rows;
+ * 500: the 8-bit linear layers and rs_residual_norm_fwd, what rs_pack_weights writes as in 400). */
 RS_API int32_t rs_version(void);
 
 /* Host string (static storage): the tile configurations the matrix kernels were built with.
@@ -259,7 +259,7 @@ RS_API rs_status rs_grid_token_prune(const void *f_out, const void *f_in, const 
  * Eqs. (5),(6): QKV, output projection, fc1, fc2; the O(N C^2) term of Sec. 3.1):
  *     out = epilogue(a @ W + bias)
  *   RS_EPI_BIAS       out = a W + bias
- *   RS_EPI_BIAS_GELU  out = GELU(a W + bias)          (exact-erf GELU)
+ *   RS_EPI_BIAS_GELU  out = GELU(a W + bias)          (the erf GELU; RS_BF16: a fit, at most 2.6e-5 + 2.9e-9 |x| off)
  *   RS_EPI_BIAS_RES   out = a W + bias + res
  *   a : [M, K].   out, res : [M, N]; out must not alias a.   bias : [N] or NULL.
  *   w : RS_F32: the [K, N] matrix as is.  RS_BF16: the [N, K] re-layout written by
@@ -276,15 +276,15 @@ RS_API rs_status rs_linear_fwd(const void *a, const void *w, const void *bias, c
 /*
  * Linear layers in 8-bit integers (W8A8): integers with one scale for each token (row of the activations) and each output channel
  * (column of the weights),
- *     out[m, n] = epilogue( (sum_k a[m, k] w[k, n]) * a_scale[m] * w_scale[n] + bias[n] )
- * the sum exact in 32-bit integers, all behind it in fp32, rounded to the output type once.  Epilogues as in rs_linear_fwd; GELU in bf16
+ *     out[m, n] = epilogue( (sum_k a[m, k] w[k, n]) * (a_scale[m] * w_scale[n]) + bias[n] )
+ * the sum exact in 32-bit integers, all behind it in fp32 and as the brackets have it, rounded to the output type once.  Epilogues as in rs_linear_fwd; GELU in bf16
  * is off by less than that rounding wherever it is 1e-18 or more.
  *
  * rs_quantize_rows forms 8-bit rows from fp32 or bf16 ones, symmetric about zero:
  *     scale[m] = max(max_k |x[m, k]| * (1 / 127), FLT_MIN),   q[m, k] = round(x[m, k] * (1 / scale[m]))
  *   each operation in fp32, halves to even: the same integers whatever ran.  A row that holds an infinity or a NaN gets scale NaN
  *   and zeros, so that a layer's output row is NaN.
- *   x : element (m, k) at m * ldx + k (elements; ldx >= K).   q : (m, k) at m * ldq + k; ldq >= K, a multiple of 16.
+ *   x : element (m, k) at m * ldx + k (elements; ldx >= K).   q : (m, k) at m * ldq + k; ldq >= K, a multiple of 16.   K <= 131071.
  *   Bytes K .. (K rounded up to 16) - 1 of a row of q are written as zeros, those behind them are left alone.   scale : float [M].
  * rs_quantize_columns does the same to the columns of a weight matrix w [K, N] (fp32 or bf16): q [K, N], scale [N].
  * rs_pack_linear_i8 lays weights q [K, N] (any int8 values) out as the kernels read them: rs_packed_linear_i8_size(K, N) bytes
@@ -345,7 +345,7 @@ RS_API rs_status rs_residual_norm_fwd(const rs_residual_norm_cfg *cfg, const rs_
  * One pre-LN encoder block followed by representation-shift pruning
  * (Eqs. (5),(6) and case (ii) of "Operation choice", Sec. 3.3):
  *     x1   = SA(LN(x)) + x             SA = fused attention + output projection
- *     mlp  = W2 GELU(W1 LN(x1) + b1) + b2        (exact-erf GELU)
+ *     mlp  = W2 GELU(W1 LN(x1) + b1) + b2        (the erf GELU, in RS_BF16 as in rs_linear_fwd)
  *     xhat = mlp + x1
  *     scores[b, i] = D(f_out[b, i, :], f_in[b, i, :])   pair by cfg->op (default: mlp, x1),
  *                                                        distance by cfg->dist (default L2)

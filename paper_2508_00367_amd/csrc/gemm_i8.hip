@@ -1,4 +1,4 @@
-// Linear layers in 8-bit integers (W8A8): out = epi((sum_k a[m,k] w[k,n]) a_scale[m] w_scale[n] + bias[n]), the sums exact in
+// Linear layers in 8-bit integers (W8A8): out = epi((sum_k a[m,k] w[k,n]) (a_scale[m] w_scale[n]) + bias[n]), the sums exact in
 // int32 (v_mfma_i32_32x32x32_i8), everything behind them in fp32, rounded once.
 //
 // Weights are packed in fragment order, [Np / 32][Kp / 32] fragments of 32 features x 32 k, 1 KB each, lane l's 16 bytes in

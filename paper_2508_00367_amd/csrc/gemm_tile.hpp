@@ -7,12 +7,13 @@
 namespace rs {
 
 // Exact-erf GELU x * Phi(x) for the bf16 epilogue: Phi(x) = sigmoid(x (a + b x^2 + c x^4)) with
-// (a, b, c) fitted (minimax over [-9, 9]) to the erf form; max |error| of x * Phi(x) is 2.5e-5,
+// (a, b, c) fitted (minimax over [-9, 9]) to the erf form; max |error| of x * Phi(x) is 2.6e-5,
 // below half a bf16 ulp of every output larger than 6e-3.  7 plain + 2 transcendental ops per
 // element (libm erff: ~40) -- it matters: the fc1 epilogue runs M * Dm of them and plain ALU
 // work does not overlap with the matrix cores on this chip.  The polynomial argument is
-// clamped to [-10, 10] (it changes sign near |x| = 11); beyond that the sigmoid is 0 or 1 in
-// fp32 anyway.  Constants carry the factor -log2(e) for v_exp_f32.
+// clamped to [-10, 10] (it changes sign near |x| = 11); above, the sigmoid is 1 in fp32, below it stays at
+// 2.9e-9 (-1e5 gives -2.9e-4).  The error is one of magnitude: in the tail it is much of the value, 3.6 % at -4 and
+// as large as it at -6.  Constants carry the factor -log2(e) for v_exp_f32.
 __device__ __forceinline__ float gelu_sp(float x) {
     const float xc = __builtin_amdgcn_fmed3f(x, -10.0f, 10.0f);
     const float x2 = xc * xc;
