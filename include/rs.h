@@ -284,14 +284,15 @@ RS_API rs_status rs_linear_fwd(const void *a, const void *w, const void *bias, c
  *     scale[m] = max(max_k |x[m, k]| * (1 / 127), FLT_MIN),   q[m, k] = round(x[m, k] * (1 / scale[m]))
  *   each operation in fp32, halves to even: the same integers whatever ran.  A row that holds an infinity or a NaN gets scale NaN
  *   and zeros, so that a layer's output row is NaN.
- *   x : element (m, k) at m * ldx + k (elements; ldx >= K).   q : (m, k) at m * ldq + k; ldq >= K, a multiple of 16.   K <= 131071.
+ *   x : element (m, k) at m * ldx + k (elements; ldx >= K).   q : (m, k) at m * ldq + k; ldq >= K, a multiple of 16.   K <= 131071,
+ *       ldx and ldq < 2^29, M < 2^31.
  *   Bytes K .. (K rounded up to 16) - 1 of a row of q are written as zeros, those behind them are left alone.   scale : float [M].
  * rs_quantize_columns does the same to the columns of a weight matrix w [K, N] (fp32 or bf16): q [K, N], scale [N].
  * rs_pack_linear_i8 lays weights q [K, N] (any int8 values) out as the kernels read them: rs_packed_linear_i8_size(K, N) bytes
  *   (0 for sizes that rs_linear_i8_fwd refuses), every one of them written.  Layout of this library version, as rs_pack_weights.
  * rs_linear_i8_fwd:  (K <= 131071: sums of that many products of 8-bit integers stay below 2^31)
- *   a : int8 (m, k) at m * lda + k, lda >= K and a multiple of 16; all M rows have lda bytes of memory.  Bytes behind column K
- *       may hold anything.        a_scale : float [M].       w : packed weights.      w_scale : float [N].
+ *   a : int8 (m, k) at m * lda + k, lda >= K and a multiple of 16, at most 2^21; all M rows have lda bytes of memory.  Bytes behind
+ *       column K may hold anything.        a_scale : float [M].       w : packed weights.      w_scale : float [N].
  *   bias : [N] or NULL;  res : [M, N] for RS_EPI_BIAS_RES;  out : [M, N], all in `dtype`.  out may be res; it must not overlap
  *       anything else.            K <= 131071, N <= 2^20, both otherwise any size; M < 2^31.
  * a_scale and scale must be 4-byte aligned, everything else 16-byte.  No workspace.  Deterministic.
@@ -317,7 +318,7 @@ RS_API rs_status rs_linear_i8_fwd(const int8_t *a, int64_t lda, const float *a_s
  *   x : [B, N, D], the residual stream.      f : [B, N, D], the branch's output, or NULL (no branch: y = x_scale * x).
  *   y, u : [B, N, D] out, each may be NULL.
  *   u_q, u_scale : u as 8-bit rows for rs_linear_i8_fwd by the rule of rs_quantize_rows (from u in fp32): int8 [B * N] rows of
- *       ldq bytes (ldq >= D, a multiple of 16) and float [B * N]; both or neither NULL.  At least one of y, u, u_q is wanted.
+ *       ldq bytes (ldq >= D, a multiple of 16, < 2^29; bytes behind column D as there) and float [B * N]; both or neither NULL.  At least one of y, u, u_q is wanted.
  *   y may be x, u may be f; otherwise no output overlaps anything.
  * Vectors (rs_residual_norm_weights, element type cfg->dtype, NULL: g and gate 1, the others 0): post_g, post_b, pre_g and
  *   pre_b are [D]; gate is read at image * gate_stride, mod_scale and mod_shift at image * mod_stride (elements; 0: one

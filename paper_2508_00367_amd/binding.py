@@ -312,7 +312,8 @@ def _here(*tensors) -> None:
 # The calls below can be short on the GPU: their checks look every tensor up once, 2.1 us of host time a call beside the library's 3.4
 # (3.1 with every check on its own).
 def rs_quantize_rows(x, q, scale, stream=None) -> None:
-    """x [M, K] (rows any distance apart) -> q int8 [M, K] in rows a multiple of 16 bytes apart, scale float [M]."""
+    """x [M, K] (rows any distance apart) -> q int8 [M, K] in rows a multiple of 16 bytes apart, scale float [M].  What lies behind a
+    row of q up to a multiple of 16 bytes is set to zero."""
     shape = x.shape
     M, K = shape
     ldx, cx = x.stride()

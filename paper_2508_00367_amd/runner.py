@@ -127,7 +127,7 @@ class EncoderBlockI8:
 
     `w`: name -> device tensor: the twelve tensors of rs_block_weights (biases, ln*_g and ln*_b may be missing) and, for encoders that
     have them, post1_g, post1_b, gate1, post2_g, post2_b, gate2, all [D].  `norm`, `post`: RS_NORM_* in front of the
-    branches and behind them.  One object serves one stream at a time."""
+    branches and behind them.  One object serves one stream at a time, the one it was made on or one that has waited for that."""
 
     def __init__(self, B: int, N: int, D: int, H: int, Dm: int, w: dict, n_prefix: int, n_keep: int, norm=rs.RS_NORM_LAYER,
                  post=rs.RS_NORM_NONE, eps: float = 1e-6, x_scale: float = 1.0, f_scale: float = 1.0, dist=rs.RS_DIST_L2):
