@@ -4,11 +4,15 @@
 // A row's f, then y, then u stay in registers between the steps; y goes into the second norm as it is in fp32, unrounded.
 // Variances are taken over the deviations from the mean.
 // Bound by reading x and f and writing y and u once, at the rate of a copy (5.1 TB/s): 4 x 4097 x 1024 fp32 with every vector 51 us, 5.3 TB/s; 256 x
-// 197 x 768 bf16 with one norm 56 us, 5.5 TB/s; with two norms and 8-bit rows (a third of the stores) 61-68 us, 4.0-4.4 TB/s: about 40 ALU instructions
+// 197 x 768 bf16 with one norm or two 61 us, 5.1 TB/s; with two norms and 8-bit rows (a third of the stores) 57 us, 4.7 TB/s, one call behind the other, and
+// 69-72 between the products of 8-bit layers, whose output is still on its way to memory: about 40 ALU instructions
 // a value then.  What it took: x and f requested together before anything is summed; every lane with work (below); vectors
-// through resources, whose scalar addresses leave the registers to the rows (161 -> 125, four waves per SIMD; forced lower, they spill: 107 us); fp32 in
-// pieces of 4 channels, so that neighbouring lanes' pieces lie side by side (58 -> 51); stores through the L2 (60 -> 56) where rows are whole lines,
-// and left to the L2 to join where they are not (8 x 4097 x 4040 fp32 474 -> 389, x 1000 bf16 65 -> 60).
+// through resources, whose scalar addresses leave the registers to the rows (bf16 in three pieces 161 -> 125, four waves per SIMD; forced lower, they
+// spill: 107 us); fp32 in pieces of 4 channels, so that neighbouring lanes' pieces lie side by side (58 -> 51); stores through the L2 where rows are whole
+// lines (4 us of 60), and left to the L2 to join where they are not (8 x 4097 x 4040 fp32 474 -> 389, x 1000 bf16 65 -> 58).
+// What it costs: up to eleven resources of four scalars each, 20 to 64 of which go to lanes of vector registers and back; four pieces a lane take 131
+// registers and more, three waves per SIMD.  fp32 rows of more than 8192 channels, 1024 lanes to a row, have 128 registers and keep
+// 80 bytes a lane in scratch memory: 4097 x 16384 242 us, 4.4 TB/s (bf16 into 8-bit rows, 512 lanes, 151 us, 3.1 TB/s).
 #include "quantize.hpp"
 
 namespace rs {
