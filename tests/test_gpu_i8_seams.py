@@ -95,3 +95,23 @@ def test_norm_rows_of_a_second_pass_many_a_wave(dtype):
         ry, ru, ey, eu = reference(x[lo:hi], f[lo:hi], {k: a[lo:hi] for k, a in v.items()}, "rms", "layer", True, 0.5, 2.0)
         within(y[lo:hi], ry, ey, dtype)
         within(u[lo:hi], ru, eu, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N", [(5, 1000), (41, 1)])
+def test_vectors_of_images_as_far_apart_as_they_may_be(B, N, dtype):
+    """2^24 elements from image to image: a wave whose rows are of two images reaches both."""
+    D, stride = 64, 1 << 24
+    _say("residual_norm", B, N, "stride 2^24", dtype)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    t = lambda *s, std=1.0: torch.empty(*s, dtype=DT[dtype], device="cuda").normal_(0.0, std, generator=g)  # noqa: E731
+    far = torch.full((B, stride), float("nan"), dtype=DT[dtype], device="cuda")
+    far[:, :3 * D] = t(B, 3 * D, std=0.4)
+    x, f, v = t(B, N, D), t(B, N, D), dict(gate=far[:, :D], mod_scale=far[:, D:2 * D], mod_shift=far[:, 2 * D:3 * D])
+    cfg = rs.make_residual_norm_cfg(B, N, D, DT[dtype], rs.RS_NORM_RMS, rs.RS_NORM_LAYER, 1e-6, 1e-5, 0.5, 2.0, stride, stride)
+    y, u = torch.empty_like(x), torch.empty_like(x)
+    rs.rs_residual_norm_fwd(cfg, rs.make_residual_norm_weights(v), x, f, y, u)
+    ry, ru, ey, eu = reference(x, f, v, "rms", "layer", True, 0.5, 2.0)
+    within(y, ry, ey, dtype)
+    within(u, ru, eu, dtype)
