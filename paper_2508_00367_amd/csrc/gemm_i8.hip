@@ -22,8 +22,8 @@ size_t packed_i8_size(int K, int N) { return align_up((size_t)N, 64) * align_up(
 // log2 Phi(-a) over 0 <= a <= 9 (minimax, with weights 1000 times smaller at 9 than at 0).  At most 6.2e-7 off; of Phi(-a), 8e-6 up to
 // a = 2, 2e-5 to 4, 1.4e-4 to 6, 1.7e-3 to 9: under half a step of bf16 (2^-9 .. 2^-8) wherever |x| Phi(-|x|) >= 1e-18.  Beyond, q only falls, and
 // the product goes to 0 as it should.  A NaN stays one; the largest finite number in |x|'s place keeps an infinity from meeting the 0.
-// 16388 x 1024 -> 4096 takes 86-89 us with it, in turn with the sigmoid of a fitted cubic that the bf16 layers of gemm.hip have as long (2.6e-5 off:
-// at -4 3.6 % of the value, as much as the value at -6), 93 with degree 10 (1.2e-7 off).
+// 16388 x 1024 -> 4096 takes 86-91 us by the run, and 84-89 with the sigmoid that the bf16 layers of gemm.hip have (2.6e-5 off: at -4 3.6 % of the value,
+// at -6 as much as the value); degree 10 (1.2e-7 off) takes 4 us more.
 __device__ __forceinline__ float gelu_tail(float x) {
     const float a = fabsf(x);
     float q = fmaf(-1.480356e-6f, a, 5.4427055e-5f);
